@@ -71,6 +71,11 @@ extern "C" {
 #define OC_CONV_TRUNCATED 4 /* the supplement's efficient convolution (constant part + truncated
                               kernels at boundary voxels), VALU; oc_conv3x3x3_ex only */
 
+/* Element types of the sequence operators (oc_attention ...). */
+#define OC_F32 0
+#define OC_F16 1
+#define OC_BF16 2
+
 /*
  * Header-only helpers on one shallow octree's bit string t[4] (layout
  * above).  They compile as plain C on the host and, inside a HIP
@@ -475,6 +480,58 @@ int oc_points_average(const int32_t* rows, int64_t n_pts, const float* feat, int
  * Exact (integer counts). */
 int oc_points_vote(const int32_t* rows, int64_t n_pts, const int32_t* labels, int n_labels,
                    int64_t n_leaves, int32_t* out, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Sequence operators.  The leaf rows of a batch are a packed array of
+ * sequences: sample i owns rows prefix[i * gd * gh * gw] up to
+ * prefix[(i + 1) * gd * gh * gw].  These operators work on such arrays, in
+ * float, IEEE half or bfloat16 (OC_F32, OC_F16, OC_BF16), with sums, softmax
+ * statistics and norms in 32 bits or more.
+ */
+
+/*
+ * Attention over packed sequences with grouped heads:
+ *   lse[i][h]  = log sum_j exp(scale q[i][h].k[j][g]),  g = h / (heads / kv_heads),
+ *   out[i][h]  = sum_j exp(scale q[i][h].k[j][g] - lse[i][h]) v[j][g]
+ * over the keys j of row i's own sequence; with causal != 0 over those that
+ * are not later than it, the last query standing beside the last key (row i
+ * of lq queries sees the first i + 1 + lk - lq of lk keys).  A row that sees
+ * no key gives out = 0 and lse = -inf.
+ *   q: [n_q][heads][dim], k, v: [n_k][kv_heads][dim], of type dtype; element
+ *   strides of rows and heads are given (dim is contiguous), so that slices
+ *   of one projection's output serve as they are.  Pointers and strides must
+ *   be multiples of 16 bytes, dim a multiple of 8 in [8, 128], heads a
+ *   multiple of kv_heads, scale positive.
+ *   q_off, k_off: int64 [n_seq + 1], sequence s has query rows
+ *   q_off[s] .. q_off[s + 1] - 1 and key rows k_off[s] ..; they start at 0,
+ *   end at n_q and n_k and do not decrease (values outside are clamped; rows
+ *   of no sequence are not written).  NULL (n_seq 1): one sequence.
+ *   k_len: int64 [n_seq], the keys of sequence s are the first k_len[s] rows
+ *   of its range (a cache that is filled in part); NULL: all of it.
+ *   out: [n_q][heads][dim] of type dtype, lse: float [n_q][heads].
+ * Where the rows are too few to fill the device the keys are split and
+ * the parts joined, in a fixed order: results do not vary from run to run.
+ */
+int oc_attention_workspace(int64_t n_q, int64_t n_k, int n_seq, int heads, int kv_heads, int dim, size_t* bytes);
+int oc_attention(const void* q, int64_t q_row, int64_t q_head, const void* k, int64_t k_row, int64_t k_head,
+                 const void* v, int64_t v_row, int64_t v_head, const int64_t* q_off, const int64_t* k_off,
+                 const int64_t* k_len, int n_seq, int64_t n_q, int64_t n_k, int heads, int kv_heads, int dim,
+                 int dtype, float scale, int causal, void* out, float* lse, void* ws, size_t ws_bytes,
+                 void* stream);
+
+/* Gradients of oc_attention from dout [n_q][heads][dim], with the out and lse
+ * of the forward call: dq [n_q][heads][dim], dk, dv [n_k][kv_heads][dim], all
+ * contiguous and of type dtype.  The gradients of a shared key/value head are
+ * the sums over its group, added up in a fixed order.  Keys must fill their
+ * ranges (no k_len). */
+int oc_attention_backward_workspace(int64_t n_q, int64_t n_k, int n_seq, int heads, int kv_heads, int dim,
+                                    size_t* bytes);
+int oc_attention_backward(const void* q, int64_t q_row, int64_t q_head, const void* k, int64_t k_row,
+                          int64_t k_head, const void* v, int64_t v_row, int64_t v_head, const void* out,
+                          const float* lse, const void* dout, const int64_t* q_off, const int64_t* k_off,
+                          int n_seq, int64_t n_q, int64_t n_k, int heads, int kv_heads, int dim, int dtype,
+                          float scale, int causal, void* dq, void* dk, void* dv, void* ws, size_t ws_bytes,
+                          void* stream);
 
 #ifdef __cplusplus
 }

@@ -1,4 +1,5 @@
 // C ABI entry points: host-side argument checks, workspace carving, launches.
+#include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
 #include <stdlib.h>
@@ -8,6 +9,7 @@
 #include <string>
 
 #include "../../include/octnet_hip.h"
+#include "oc_attention.h"
 #include "oc_internal.h"
 
 namespace {
@@ -644,6 +646,133 @@ int oc_points_vote(const int32_t* rows, int64_t n_pts, const int32_t* labels, in
   OC_CHECK_HIP(oci::launch_label_vote(rows, n_pts, labels, n_labels, n_leaves, out,
                                       static_cast<uint32_t*>(ws), as_stream(stream)),
                "oc_points_vote");
+  return OC_OK;
+}
+
+namespace {
+
+int type_bytes(int dtype) { return dtype == OC_F32 ? 4 : 2; }
+
+bool type_ok(int dtype) { return dtype == OC_F32 || dtype == OC_F16 || dtype == OC_BF16; }
+
+bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+// Sizes that the attention kernels' 32-bit row numbers and grids hold.
+int attention_sizes(const char* who, int64_t n_q, int64_t n_k, int n_seq, int heads, int kv_heads, int dim) {
+  if (n_q < 0 || n_k < 0 || n_seq <= 0) return fail(OC_EINVAL, "%s: negative size, or no sequence", who);
+  if (heads <= 0 || kv_heads <= 0 || heads % kv_heads)
+    return fail(OC_EINVAL, "%s: %d heads for %d key heads", who, heads, kv_heads);
+  if (dim < 8 || dim > 128 || dim % 8) return fail(OC_EINVAL, "%s: head size %d is no multiple of 8 in [8, 128]", who, dim);
+  const int64_t most = (1LL << 31) - 256;
+  if (n_q > most / heads || n_k > most / kv_heads) return fail(OC_EOVERFLOW, "%s: more than 2^31 rows", who);
+  const int64_t rows = n_q * (heads / kv_heads) > n_k ? n_q * (heads / kv_heads) : n_k;
+  if ((rows / 32 + n_seq) > most / kv_heads / 128) return fail(OC_EOVERFLOW, "%s: too many row tiles", who);
+  return OC_OK;
+}
+
+int attention_args(const char* who, const void* q, int64_t q_row, int64_t q_head, const void* k, int64_t k_row,
+                   int64_t k_head, const void* v, int64_t v_row, int64_t v_head, const int64_t* q_off,
+                   const int64_t* k_off, int n_seq, int64_t n_q, int64_t n_k, int heads, int kv_heads, int dim,
+                   int dtype, float scale, int causal, oci::AttnArgs* a) {
+  const int rc = attention_sizes(who, n_q, n_k, n_seq, heads, kv_heads, dim);
+  if (rc != OC_OK) return rc;
+  if (!type_ok(dtype)) return fail(OC_EINVAL, "%s: bad type %d", who, dtype);
+  if ((n_q > 0 && !q) || (n_k > 0 && (!k || !v))) return fail(OC_EINVAL, "%s: null pointer", who);
+  if (n_seq > 1 && (!q_off || !k_off)) return fail(OC_EINVAL, "%s: %d sequences without offsets", who, n_seq);
+  if (!(scale > 0.f) || !isfinite(scale)) return fail(OC_EINVAL, "%s: scale %g is not positive", who, scale);
+  const int64_t strides[] = {q_row, q_head, k_row, k_head, v_row, v_head};
+  for (int64_t x : strides)
+    if (x < 0 || x * type_bytes(dtype) % 16) return fail(OC_EINVAL, "%s: stride %lld is no multiple of 16 bytes", who, (long long)x);
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v)) return fail(OC_EINVAL, "%s: pointer not aligned to 16 bytes", who);
+  *a = oci::AttnArgs();
+  a->q = q; a->k = k; a->v = v;
+  a->q_row = q_row; a->q_head = q_head; a->k_row = k_row; a->k_head = k_head; a->v_row = v_row; a->v_head = v_head;
+  a->q_off = q_off; a->k_off = k_off;
+  a->n_seq = n_seq; a->n_q = n_q; a->n_k = n_k;
+  a->heads = heads; a->kv_heads = kv_heads; a->dim = dim;
+  a->scale = scale; a->causal = causal ? 1 : 0;
+  a->n_split = 1;
+  oci::attention_set_group(a);
+  return OC_OK;
+}
+
+}  // namespace
+
+int oc_attention_workspace(int64_t n_q, int64_t n_k, int n_seq, int heads, int kv_heads, int dim, size_t* bytes) {
+  g_last_error.clear();
+  if (!bytes) return fail(OC_EINVAL, "oc_attention_workspace: null pointer");
+  const int rc = attention_sizes("oc_attention_workspace", n_q, n_k, n_seq, heads, kv_heads, dim);
+  if (rc != OC_OK) return rc;
+  const int n = oci::attention_splits(n_q, n_k, n_seq, heads, kv_heads);
+  const size_t rows = (size_t)n_q * heads;
+  *bytes = n > 1 ? oci::align256(4 * n * rows * dim) + oci::align256(4 * n * rows) : 0;
+  return OC_OK;
+}
+
+int oc_attention(const void* q, int64_t q_row, int64_t q_head, const void* k, int64_t k_row, int64_t k_head,
+                 const void* v, int64_t v_row, int64_t v_head, const int64_t* q_off, const int64_t* k_off,
+                 const int64_t* k_len, int n_seq, int64_t n_q, int64_t n_k, int heads, int kv_heads, int dim,
+                 int dtype, float scale, int causal, void* out, float* lse, void* ws, size_t ws_bytes,
+                 void* stream) {
+  g_last_error.clear();
+  oci::AttnArgs a;
+  const int rc = attention_args("oc_attention", q, q_row, q_head, k, k_row, k_head, v, v_row, v_head, q_off, k_off,
+                                n_seq, n_q, n_k, heads, kv_heads, dim, dtype, scale, causal, &a);
+  if (rc != OC_OK) return rc;
+  if (n_q == 0) return OC_OK;
+  if (!out || !lse) return fail(OC_EINVAL, "oc_attention: null pointer");
+  if (!aligned16(out)) return fail(OC_EINVAL, "oc_attention: pointer not aligned to 16 bytes");
+  a.k_len = k_len;
+  a.out = out;
+  a.lse = lse;
+  a.n_split = oci::attention_splits(n_q, n_k, n_seq, heads, kv_heads);
+  if (a.n_split > 1) {
+    const size_t rows = (size_t)n_q * heads, part = oci::align256(4 * a.n_split * rows * dim);
+    if (!ws || ws_bytes < part + oci::align256(4 * a.n_split * rows))
+      return fail(OC_EWORKSPACE, "oc_attention: workspace too small");
+    if (!aligned16(ws)) return fail(OC_EINVAL, "oc_attention: workspace not aligned to 16 bytes");
+    a.part = static_cast<float*>(ws);
+    a.part_lse = reinterpret_cast<float*>(static_cast<char*>(ws) + part);
+  }
+  OC_CHECK_HIP(oci::launch_attention(a, dtype, as_stream(stream)), "oc_attention");
+  return OC_OK;
+}
+
+int oc_attention_backward_workspace(int64_t n_q, int64_t n_k, int n_seq, int heads, int kv_heads, int dim,
+                                    size_t* bytes) {
+  g_last_error.clear();
+  if (!bytes) return fail(OC_EINVAL, "oc_attention_backward_workspace: null pointer");
+  const int rc = attention_sizes("oc_attention_backward_workspace", n_q, n_k, n_seq, heads, kv_heads, dim);
+  if (rc != OC_OK) return rc;
+  *bytes = 2 * oci::align256(4 * (size_t)n_q * heads);
+  return OC_OK;
+}
+
+int oc_attention_backward(const void* q, int64_t q_row, int64_t q_head, const void* k, int64_t k_row,
+                          int64_t k_head, const void* v, int64_t v_row, int64_t v_head, const void* out,
+                          const float* lse, const void* dout, const int64_t* q_off, const int64_t* k_off,
+                          int n_seq, int64_t n_q, int64_t n_k, int heads, int kv_heads, int dim, int dtype,
+                          float scale, int causal, void* dq, void* dk, void* dv, void* ws, size_t ws_bytes,
+                          void* stream) {
+  g_last_error.clear();
+  oci::AttnArgs a;
+  const int rc = attention_args("oc_attention_backward", q, q_row, q_head, k, k_row, k_head, v, v_row, v_head, q_off,
+                                k_off, n_seq, n_q, n_k, heads, kv_heads, dim, dtype, scale, causal, &a);
+  if (rc != OC_OK) return rc;
+  if ((n_q > 0 && (!out || !lse || !dout || !dq)) || (n_k > 0 && (!dk || !dv)))
+    return fail(OC_EINVAL, "oc_attention_backward: null pointer");
+  if (!aligned16(out) || !aligned16(dout) || !aligned16(dq) || !aligned16(dk) || !aligned16(dv))
+    return fail(OC_EINVAL, "oc_attention_backward: pointer not aligned to 16 bytes");
+  const size_t part = oci::align256(4 * (size_t)n_q * heads);
+  if (n_q > 0 && (!ws || ws_bytes < 2 * part)) return fail(OC_EWORKSPACE, "oc_attention_backward: workspace too small");
+  if (!aligned16(ws)) return fail(OC_EINVAL, "oc_attention_backward: workspace not aligned to 16 bytes");
+  a.out = const_cast<void*>(out);
+  a.lse = const_cast<float*>(lse);
+  a.dout = dout;
+  a.dq = dq; a.dk = dk; a.dv = dv;
+  a.delta = static_cast<float*>(ws);
+  a.lse2 = reinterpret_cast<float*>(static_cast<char*>(ws) + part);
+  OC_CHECK_HIP(oci::launch_attention_backward(a, dtype, as_stream(stream)), "oc_attention_backward");
   return OC_OK;
 }
 

@@ -1,0 +1,823 @@
+// Attention over packed sequences: forward, gradients, and the join of key
+// ranges when there are few rows.
+//
+//   out_i = sum_j p_ij v_j,  p_ij = exp(scale q_i.k_j - lse_i),
+//   lse_i = log sum_j exp(scale q_i.k_j)      over the keys j that row i sees.
+//
+// Rows.  The group of query heads that shares one key/value head is packed:
+// packed row r of a sequence is query r / group of head r % group.  A tile of
+// rows reads each key once for the whole group, a single query still fills
+// `group` rows of a tile, and the sums over shared heads in dK and dV are
+// ordinary sums over rows, in a fixed order.
+//
+// Matrix products.  Every product is formed transposed so that the second
+// one takes the first one's accumulator as it stands: with S^T = K Q^T a lane
+// of the 32x32 accumulator holds one query (column lane % 32) and 16 keys, and
+// as the order of a contraction is free, those 16 values in their order are
+// already the B operand of O^T = V^T P^T.  The A operand takes its keys in
+// the same order: element i of lane half h is key 8 (i / 4) + 4 h + i % 4 of
+// each 16.  Softmax statistics are per lane, with one exchange between lane
+// halves per tile.  16-bit A operands over the row index of an LDS tile come
+// from the transposing LDS read; 32-bit ones are read one by one.
+#include "oc_attention.h"
+
+namespace oci {
+namespace {
+
+using f32x4 = __attribute__((ext_vector_type(4))) float;
+using f32x8 = __attribute__((ext_vector_type(8))) float;
+using f32x16 = __attribute__((ext_vector_type(16))) float;
+using bf16x8 = __attribute__((ext_vector_type(8))) __bf16;
+using f16x8 = __attribute__((ext_vector_type(8))) _Float16;
+using i16x4 = __attribute__((ext_vector_type(4))) short;
+using u32x4 = __attribute__((ext_vector_type(4))) uint32_t;
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+#define OC_INF __builtin_inff()
+
+// Fragment of eight contraction elements per lane, and one 32x32 product over
+// 16 of them: one instruction for 16-bit types; for float eight
+// instructions that contract elements (i of half 0, i of half 1) each.
+template <class T>
+struct Frag;
+template <>
+struct Frag<__bf16> {
+  using type = bf16x8;
+  static constexpr int kShift = 0;
+};
+template <>
+struct Frag<_Float16> {
+  using type = f16x8;
+  // Normalised probabilities of long sequences would fall below float16's
+  // normal range (2^-14); the gradients carry them times 2^12.
+  static constexpr int kShift = 12;
+};
+template <>
+struct Frag<float> {
+  using type = f32x8;
+  static constexpr int kShift = 0;
+};
+template <class T>
+using frag_t = typename Frag<T>::type;
+
+__device__ __forceinline__ f32x16 mma(bf16x8 a, bf16x8 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mma(f16x8 a, f16x8 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mma(f32x8 a, f32x8 b, f32x16 c) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], b[i], c, 0, 0, 0);
+  return c;
+}
+
+__device__ __forceinline__ int lane() { return (int)(threadIdx.x & 63); }
+__device__ __forceinline__ int wave() { return __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)); }
+
+// x of this lane and of the lane 32 away.
+__device__ __forceinline__ float half_max(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float half_sum(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+__device__ __forceinline__ f32x16 zero16() {
+  f32x16 z;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) z[i] = 0.f;
+  return z;
+}
+
+// The eight accumulator values from `first` on as a fragment.
+template <class T>
+__device__ __forceinline__ frag_t<T> to_frag(const f32x16& c, int first) {
+  f32x8 x;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = c[first + i];
+  return __builtin_convertvector(x, frag_t<T>);
+}
+
+// A tile of R rows of up to D elements in LDS: rows of P elements (P the
+// power of two from D up) in 16-byte chunks, chunk c of row r at position
+// c ^ swizzle(r).  Eight consecutive rows at one chunk (a row-wise fragment
+// read) and four rows at two neighbouring chunks (a transposing read) then
+// touch every bank once.
+template <class T, int D, int R>
+struct Tile {
+  static constexpr int kPer = 16 / (int)sizeof(T);        // elements per chunk
+  static constexpr int P = D <= 32 ? 32 : D <= 64 ? 64 : 128;
+  static constexpr int kChunks = P / kPer;                // chunks per row: 4, 8, 16 or 32
+  static constexpr int kBytes = R * P * (int)sizeof(T);
+
+  static __device__ __forceinline__ int swizzle(int r) {
+    return kChunks >= 8 ? (((r & 3) << 1) | ((r >> 2) & 1)) : ((r & 2) | ((r >> 2) & 1));
+  }
+  static __device__ __forceinline__ int at(int r, int chunk) {
+    return (r * kChunks + (chunk ^ swizzle(r))) * 16;
+  }
+
+  // Elements 8 h .. 8 h + 7 past `col` of row `row + lane % 32`.
+  static __device__ __forceinline__ frag_t<T> rows(const char* t, int row, int col) {
+    const int r = row + (lane() & 31), h = lane() >> 5;
+    if constexpr (sizeof(T) == 2) {
+      const u32x4 x = *(const u32x4*)(t + at(r, col / 8 + h));
+      return __builtin_bit_cast(frag_t<T>, x);
+    } else {
+      const f32x4 x = *(const f32x4*)(t + at(r, col / 4 + 2 * h));
+      const f32x4 y = *(const f32x4*)(t + at(r, col / 4 + 2 * h + 1));
+      return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+  }
+
+  // Rows row + 8 (i / 4) + 4 h + i % 4, i = 0..7, of column col + lane % 32.
+  static __device__ __forceinline__ frag_t<T> cols(const char* t, int row, int col) {
+    const int l = lane(), h = l >> 5;
+    if constexpr (sizeof(T) == 2) {
+      // Lanes of a group of 16 read four rows of 16 elements, four elements
+      // each, and get one column each.
+      const int r = row + 4 * h + ((l >> 2) & 3), c = col + (l & 16) + 4 * (l & 3);
+      using lds4 = __attribute__((address_space(3))) i16x4;
+      const i16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(t + at(r, c / 8) + (c & 7) * 2));
+      const i16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(t + at(r + 8, c / 8) + (c & 7) * 2));
+      return __builtin_bit_cast(frag_t<T>, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+    } else {
+      const int c = col + (l & 31);
+      f32x8 x;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int r = row + 8 * (i / 4) + 4 * h + i % 4;
+        x[i] = *(const float*)(t + at(r, c / 4) + (c & 3) * 4);
+      }
+      return x;
+    }
+  }
+};
+
+// Copy of a tile from global memory through registers: load() issues the
+// reads, store() writes them to LDS.  Rows past the end and columns past the
+// head size become zero, whatever lies there in memory.
+template <class T, int D, int R, int NT>
+struct Stage {
+  using L = Tile<T, D, R>;
+  static constexpr int kN = (R * L::kChunks + NT - 1) / NT;
+  u32x4 x[kN];
+
+  // row_at(r): the address of row r's first element, or null.
+  template <class F>
+  __device__ __forceinline__ void load(int dim, F row_at) {
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+      const int n = (int)threadIdx.x + i * NT;
+      const int r = n / L::kChunks, c = (n % L::kChunks) ^ L::swizzle(r);
+      const T* p = (R * L::kChunks % NT == 0 || r < R) && c * L::kPer < dim ? row_at(r) : nullptr;
+      x[i] = p ? *(const u32x4*)(p + c * L::kPer) : u32x4{0, 0, 0, 0};
+    }
+  }
+  __device__ __forceinline__ void store(char* t) const {
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+      const int n = (int)threadIdx.x + i * NT;
+      if (R * L::kChunks % NT == 0 || n < R * L::kChunks) *(u32x4*)(t + n * 16) = x[i];
+    }
+  }
+};
+
+// ---------------------------------------------------------------------------
+// Sequences and tiles
+// ---------------------------------------------------------------------------
+
+struct Seq {
+  int64_t q0, k0;  // first query and key row
+  int lq, lk;      // queries and keys
+};
+
+// n / d for n < 2^31 (AttnArgs::div_*).
+__device__ __forceinline__ int by_group(const AttnArgs& a, int n) {
+  return (int)((__umulhi(a.div_mul, (uint32_t)n) + (uint32_t)n) >> a.div_shift);
+}
+
+// Offsets come from device memory, unchecked: clamped into the arrays, so
+// that wrong ones give wrong results and no access outside.
+__device__ __forceinline__ int64_t bounded(int64_t x, int64_t lo, int64_t hi) {
+  return x < lo ? lo : x > hi ? hi : x;
+}
+
+__device__ __forceinline__ Seq seq_of(const AttnArgs& a, int s) {
+  Seq e;
+  e.q0 = a.q_off ? bounded(a.q_off[s], 0, a.n_q) : 0;
+  const int64_t q1 = a.q_off ? bounded(a.q_off[s + 1], e.q0, a.n_q) : a.n_q;
+  e.k0 = a.k_off ? bounded(a.k_off[s], 0, a.n_k) : 0;
+  const int64_t k1 = a.k_off ? bounded(a.k_off[s + 1], e.k0, a.n_k) : a.n_k;
+  e.lq = (int)(q1 - e.q0);
+  e.lk = (int)(a.k_len ? bounded(a.k_len[s], 0, k1 - e.k0) : k1 - e.k0);
+  return e;
+}
+
+// Tiles of sequences whose lengths only the device knows: sequence s with
+// first row o owns slots o / tile + s onwards, which leaves room for
+// ceil(length / tile) tiles whatever the lengths.  Returns the sequence of
+// `slot` (64 candidates per step), and its first slot.
+__device__ __forceinline__ int seq_of_slot(const int64_t* off, int n_seq, int64_t n, int mul, int tile, int64_t slot,
+                                           int64_t* first) {
+  if (!off) {
+    *first = 0;
+    return 0;
+  }
+  int lo = 0, count = n_seq;  // the answer lies in [lo, lo + count)
+  while (count > 1) {
+    const int step = (count + 63) / 64;
+    const int s = lo + lane() * step;
+    const bool in = s < lo + count;
+    const int64_t start = in ? bounded(off[s], 0, n) * mul / tile + s : 0;
+    const int hits = __popcll(__ballot(in && start <= slot));
+    // Candidate 0 always qualifies for lo = 0; keep lo if offsets are wrong.
+    const int k = hits > 0 ? hits - 1 : 0;
+    const int left = count - k * step;
+    lo += k * step;
+    count = left < step ? left : step;
+  }
+  lo = __builtin_amdgcn_readfirstlane(lo);
+  *first = bounded(off[lo], 0, n) * mul / tile + lo;
+  return lo;
+}
+
+// Keys that packed row r of the sequence sees: the first `seen` ones.
+__device__ __forceinline__ int seen_keys(const AttnArgs& a, const Seq& e, int r) {
+  if (!a.causal) return e.lk;
+  const int n = by_group(a, r) + 1 + (e.lk - e.lq);
+  return n < 0 ? 0 : n > e.lk ? e.lk : n;
+}
+
+// Offset in elements of packed row r (relative to the sequence's and head
+// group's first element).
+__device__ __forceinline__ int64_t row_offset(const AttnArgs& a, int r, int64_t row_stride, int64_t head_stride) {
+  const int q = by_group(a, r);
+  return q * row_stride + (int64_t)(r - q * a.group) * head_stride;
+}
+
+template <class T>
+__device__ __forceinline__ u32x4 load16(const T* p) {
+  return *(const u32x4*)p;
+}
+
+// B fragment (elements col + 8 h .. of a row in global memory), zero past dim.
+template <class T>
+__device__ __forceinline__ frag_t<T> global_frag(const T* row, bool valid, int col, int dim) {
+  const int c = col + 8 * (lane() >> 5);
+  if constexpr (sizeof(T) == 2) {
+    const u32x4 x = valid && c < dim ? load16(row + c) : u32x4{0, 0, 0, 0};
+    return __builtin_bit_cast(frag_t<T>, x);
+  } else {
+    const u32x4 z = {0, 0, 0, 0};
+    const u32x4 x = valid && c < dim ? load16(row + c) : z;
+    const u32x4 y = valid && c + 4 < dim ? load16(row + c + 4) : z;
+    return __builtin_shufflevector(__builtin_bit_cast(f32x4, x), __builtin_bit_cast(f32x4, y), 0, 1, 2, 3, 4, 5, 6, 7);
+  }
+}
+
+// Stores an accumulator whose column is this lane's row: elements
+// d0 + 8 (i / 4) + 4 h + i % 4 of the row at p, times f.
+template <class T>
+__device__ __forceinline__ void store_col(T* p, const f32x16& c, int d0, int dim, float f) {
+  const int h = lane() >> 5;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int d = d0 + 8 * i + 4 * h;
+    if (d < dim) {
+      f32x4 x = {c[4 * i] * f, c[4 * i + 1] * f, c[4 * i + 2] * f, c[4 * i + 3] * f};
+      using V = __attribute__((ext_vector_type(4))) T;
+      *(V*)(p + d) = __builtin_convertvector(x, V);
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Forward
+// ---------------------------------------------------------------------------
+
+// NW waves of MT x 32 packed rows each, BN keys per step, two LDS buffers.
+template <class T, int D, int MT, int NW, int BN>
+__global__ __launch_bounds__(NW * 64) void k_attention(AttnArgs a) {
+  using L = Tile<T, D, BN>;
+  constexpr int NT = NW * 64, BM = NW * MT * 32;
+  __shared__ __attribute__((aligned(16))) char lds[2][2][L::kBytes];
+
+  const int kvh = (int)(blockIdx.x % (unsigned)a.kv_heads);
+  // Rows with the most keys first where the mask is causal.
+  const int64_t slot = (int64_t)(gridDim.x / (unsigned)a.kv_heads) - 1 - blockIdx.x / (unsigned)a.kv_heads;
+  int64_t first;
+  const int s = seq_of_slot(a.q_off, a.n_seq, a.n_q, a.group, BM, slot, &first);
+  const Seq e = seq_of(a, s);
+  const int rows = e.lq * a.group;
+  const int64_t r0_64 = (slot - first) * BM;
+  if (r0_64 < 0 || r0_64 >= rows) return;
+  const int r0 = (int)r0_64;
+
+  const int w = wave(), l32 = lane() & 31, h = lane() >> 5;
+  // Keys of this tile, and of this part where the keys are split.
+  const int last = r0 + BM < rows ? r0 + BM - 1 : rows - 1;
+  const int most = seen_keys(a, e, last);
+  int t0 = 0, t1 = (most + BN - 1) / BN;
+  if (a.n_split > 1) {
+    const int per = (t1 + a.n_split - 1) / a.n_split;
+    t0 = (int)blockIdx.y * per;
+    t1 = t0 + per < t1 ? t0 + per : t1;
+  }
+
+  const T* q = (const T*)a.q + e.q0 * a.q_row + (int64_t)kvh * a.group * a.q_head;
+  const T* k = (const T*)a.k + e.k0 * a.k_row + (int64_t)kvh * a.k_head;
+  const T* v = (const T*)a.v + e.k0 * a.v_row + (int64_t)kvh * a.v_head;
+
+  frag_t<T> qf[MT][D / 16];
+  int seen[MT], seen_min[MT], seen_max = 0;
+#pragma unroll
+  for (int m = 0; m < MT; ++m) {
+    const int w0 = r0 + (w * MT + m) * 32;  // first row of the 32
+    const int r = w0 + l32;
+    const int rr = r < rows ? r : rows - 1;
+    seen[m] = seen_keys(a, e, rr);
+    seen_min[m] = __builtin_amdgcn_readfirstlane(seen_keys(a, e, w0 < rows ? w0 : rows - 1));
+    const T* p = q + row_offset(a, rr, a.q_row, a.q_head);
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) qf[m][i] = global_frag<T>(p, true, 16 * i, a.dim);
+    const int e1 = w0 + 31 < rows ? w0 + 31 : rows - 1;
+    const int mx = w0 < rows ? seen_keys(a, e, e1) : 0;
+    seen_max = mx > seen_max ? mx : seen_max;
+  }
+  seen_max = __builtin_amdgcn_readfirstlane(seen_max);
+
+  f32x16 o[MT][D / 32];
+  float mx[MT], sum[MT];
+#pragma unroll
+  for (int m = 0; m < MT; ++m) {
+    mx[m] = -OC_INF;
+    sum[m] = 0.f;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d) o[m][d] = zero16();
+  }
+  const float c = a.scale * kLog2e;
+
+  Stage<T, D, BN, NT> ks, vs;
+  const auto load = [&](int t) {
+    ks.load(a.dim, [&](int r) { return t * BN + r < e.lk ? k + (int64_t)(t * BN + r) * a.k_row : nullptr; });
+    vs.load(a.dim, [&](int r) { return t * BN + r < e.lk ? v + (int64_t)(t * BN + r) * a.v_row : nullptr; });
+  };
+  if (t0 < t1) {
+    load(t0);
+    ks.store(lds[0][0]);
+    vs.store(lds[0][1]);
+  }
+  __syncthreads();
+  for (int t = t0; t < t1; ++t) {
+    const char* kt = lds[(t - t0) & 1][0];
+    const char* vt = lds[(t - t0) & 1][1];
+    if (t + 1 < t1) load(t + 1);
+    if (t * BN < seen_max) {
+      f32x16 x[MT][BN / 32];
+#pragma unroll
+      for (int n = 0; n < BN / 32; ++n) {
+#pragma unroll
+        for (int m = 0; m < MT; ++m) x[m][n] = zero16();
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) {
+          const frag_t<T> kf = L::rows(kt, 32 * n, 16 * i);
+#pragma unroll
+          for (int m = 0; m < MT; ++m) x[m][n] = mma(kf, qf[m][i], x[m][n]);
+        }
+      }
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        if ((t + 1) * BN > seen_min[m]) {
+#pragma unroll
+          for (int n = 0; n < BN / 32; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const int key = t * BN + 32 * n + 8 * (i / 4) + 4 * h + i % 4;
+              if (key >= seen[m]) x[m][n][i] = -OC_INF;
+            }
+        }
+        float top = x[m][0][0];
+#pragma unroll
+        for (int n = 0; n < BN / 32; ++n)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) top = fmaxf(top, x[m][n][i]);
+        top = half_max(top);
+        // The running maximum may lag the true one by up to 8 in base 2: the
+        // sums stay exact ratios, and most steps need no rescaling.
+        if (__any((top - mx[m]) * c > 8.f)) {
+          const float now = fmaxf(mx[m], top);
+          const float f = now == -OC_INF ? 1.f : __builtin_amdgcn_exp2f((mx[m] - now) * c);
+          mx[m] = now;
+          sum[m] *= f;
+#pragma unroll
+          for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[m][d][i] *= f;
+        }
+        const float off = mx[m] == -OC_INF ? 0.f : -mx[m] * c;
+#pragma unroll
+        for (int n = 0; n < BN / 32; ++n)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            x[m][n][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[m][n][i], c, off));
+            sum[m] += x[m][n][i];
+          }
+      }
+#pragma unroll
+      for (int n = 0; n < BN / 32; ++n)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          frag_t<T> pf[MT];
+#pragma unroll
+          for (int m = 0; m < MT; ++m) pf[m] = to_frag<T>(x[m][n], 8 * j);
+#pragma unroll
+          for (int d = 0; d < D / 32; ++d) {
+            const frag_t<T> vf = L::cols(vt, 32 * n + 16 * j, 32 * d);
+#pragma unroll
+            for (int m = 0; m < MT; ++m) o[m][d] = mma(vf, pf[m], o[m][d]);
+          }
+        }
+    }
+    if (t + 1 < t1) {
+      ks.store(lds[(t + 1 - t0) & 1][0]);
+      vs.store(lds[(t + 1 - t0) & 1][1]);
+    }
+    __syncthreads();
+  }
+
+#pragma unroll
+  for (int m = 0; m < MT; ++m) {
+    const int r = r0 + (w * MT + m) * 32 + l32;
+    if (r >= rows) continue;
+    const float total = half_sum(sum[m]);
+    const float f = total > 0.f || total != total ? 1.f / total : 0.f;
+    const float lse = total == 0.f ? -OC_INF : (mx[m] * c + __builtin_amdgcn_logf(total)) * kLn2;
+    const int qi = by_group(a, r);
+    const int64_t at = (e.q0 + qi) * a.heads + (int64_t)kvh * a.group + (r - qi * a.group);
+    if (a.n_split > 1) {
+      const int64_t part = (int64_t)blockIdx.y * a.n_q * a.heads + at;
+      if (h == 0) a.part_lse[part] = lse;
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d) store_col<float>(a.part + part * a.dim, o[m][d], 32 * d, a.dim, f);
+    } else {
+      if (h == 0) a.lse[at] = lse;
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d) store_col<T>((T*)a.out + at * a.dim, o[m][d], 32 * d, a.dim, f);
+    }
+  }
+}
+
+// The parts of each row weighted by exp(lse_part - lse): one wave per row.
+template <class T>
+__global__ __launch_bounds__(256) void k_attention_join(AttnArgs a) {
+  const int64_t row = (int64_t)blockIdx.x * 4 + wave(), n = a.n_q * a.heads;
+  if (row >= n) return;
+  float top = -OC_INF;
+  for (int s = 0; s < a.n_split; ++s) top = fmaxf(top, a.part_lse[s * n + row]);
+  const float base = top == -OC_INF ? 0.f : top;
+  float total = 0.f;
+  for (int s = 0; s < a.n_split; ++s) total += __expf(a.part_lse[s * n + row] - base);
+  const float f = total > 0.f || total != total ? 1.f / total : 0.f;
+  if (lane() == 0) a.lse[row] = total == 0.f ? -OC_INF : base + __logf(total);
+  for (int d = lane(); d < a.dim; d += 64) {
+    float x = 0.f;
+    for (int s = 0; s < a.n_split; ++s) {
+      const float w = __expf(a.part_lse[s * n + row] - base);
+      if (w != 0.f) x += w * a.part[(s * n + row) * a.dim + d];
+    }
+    ((T*)a.out)[row * a.dim + d] = (T)(x * f);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Gradients
+// ---------------------------------------------------------------------------
+
+// Per row: delta = sum_d dout out, and lse in base 2 (infinite where the row
+// sees no key, so that its probabilities come out zero).  16 lanes per row.
+template <class T>
+__global__ __launch_bounds__(256) void k_attention_delta(AttnArgs a) {
+  const int64_t row = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4), n = a.n_q * a.heads;
+  if (row >= n) return;
+  const T* x = (const T*)a.out + row * a.dim;
+  const T* y = (const T*)a.dout + row * a.dim;
+  constexpr int kPer = 16 / (int)sizeof(T);
+  using V = __attribute__((ext_vector_type(kPer))) T;
+  float sum = 0.f;
+  for (int d = (int)(threadIdx.x & 15) * kPer; d < a.dim; d += 16 * kPer) {
+    const V u = *(const V*)(x + d), v = *(const V*)(y + d);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) sum += (float)u[i] * (float)v[i];
+  }
+#pragma unroll
+  for (int i = 8; i; i >>= 1) sum += __shfl_xor(sum, i, 16);
+  if ((threadIdx.x & 15) == 0) {
+    a.delta[row] = sum;
+    const float lse = a.lse[row];
+    a.lse2[row] = lse == -OC_INF ? OC_INF : lse * kLog2e;
+  }
+}
+
+// dQ: waves of 32 packed rows over the keys, as the forward pass.
+//   S^T = K Q^T, dP^T = V dO^T, dS^T = P^T (dP^T - delta), dQ^T += K^T dS^T.
+template <class T, int D, int NW, int BN>
+__global__ __launch_bounds__(NW * 64) void k_attention_dq(AttnArgs a) {
+  using L = Tile<T, D, BN>;
+  constexpr int NT = NW * 64, BM = NW * 32;
+  __shared__ __attribute__((aligned(16))) char lds[2][2][L::kBytes];
+  const int kvh = (int)(blockIdx.x % (unsigned)a.kv_heads);
+  const int64_t slot = (int64_t)(gridDim.x / (unsigned)a.kv_heads) - 1 - blockIdx.x / (unsigned)a.kv_heads;
+  int64_t first;
+  const int s = seq_of_slot(a.q_off, a.n_seq, a.n_q, a.group, BM, slot, &first);
+  const Seq e = seq_of(a, s);
+  const int rows = e.lq * a.group;
+  const int64_t r0_64 = (slot - first) * BM;
+  if (r0_64 < 0 || r0_64 >= rows) return;
+  const int r0 = (int)r0_64;
+  const int w = wave(), l32 = lane() & 31, h = lane() >> 5;
+  const int last = r0 + BM < rows ? r0 + BM - 1 : rows - 1;
+  const int t1 = (seen_keys(a, e, last) + BN - 1) / BN;
+
+  const T* q = (const T*)a.q + e.q0 * a.q_row + (int64_t)kvh * a.group * a.q_head;
+  const T* k = (const T*)a.k + e.k0 * a.k_row + (int64_t)kvh * a.k_head;
+  const T* v = (const T*)a.v + e.k0 * a.v_row + (int64_t)kvh * a.v_head;
+  const int w0 = r0 + w * 32, r = w0 + l32;
+  const int rr = r < rows ? r : rows - 1;
+  const int seen = seen_keys(a, e, rr);
+  const int seen_min = __builtin_amdgcn_readfirstlane(seen_keys(a, e, w0 < rows ? w0 : rows - 1));
+  const int seen_max =
+      __builtin_amdgcn_readfirstlane(w0 < rows ? seen_keys(a, e, w0 + 31 < rows ? w0 + 31 : rows - 1) : 0);
+  const int qi = by_group(a, rr);
+  const int64_t at = (e.q0 + qi) * a.heads + (int64_t)kvh * a.group + (rr - qi * a.group);
+  const T* qp = q + row_offset(a, rr, a.q_row, a.q_head);
+  const T* dp = (const T*)a.dout + at * a.dim;
+  frag_t<T> qf[D / 16], df[D / 16];
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i) {
+    qf[i] = global_frag<T>(qp, true, 16 * i, a.dim);
+    df[i] = global_frag<T>(dp, true, 16 * i, a.dim);
+  }
+  const float lse2 = a.lse2[at], delta = a.delta[at];
+  f32x16 g[D / 32];
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d) g[d] = zero16();
+  const float c = a.scale * kLog2e;
+
+  Stage<T, D, BN, NT> ks, vs;
+  const auto load = [&](int t) {
+    ks.load(a.dim, [&](int r) { return t * BN + r < e.lk ? k + (int64_t)(t * BN + r) * a.k_row : nullptr; });
+    vs.load(a.dim, [&](int r) { return t * BN + r < e.lk ? v + (int64_t)(t * BN + r) * a.v_row : nullptr; });
+  };
+  if (t1 > 0) {
+    load(0);
+    ks.store(lds[0][0]);
+    vs.store(lds[0][1]);
+  }
+  __syncthreads();
+  for (int t = 0; t < t1; ++t) {
+    const char* kt = lds[t & 1][0];
+    const char* vt = lds[t & 1][1];
+    if (t + 1 < t1) load(t + 1);
+    if (t * BN < seen_max) {
+#pragma unroll
+      for (int n = 0; n < BN / 32; ++n) {
+        f32x16 x = zero16(), y = zero16();
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) x = mma(L::rows(kt, 32 * n, 16 * i), qf[i], x);
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) y = mma(L::rows(vt, 32 * n, 16 * i), df[i], y);
+        const bool mask = t * BN + 32 * n + 32 > seen_min;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int key = t * BN + 32 * n + 8 * (i / 4) + 4 * h + i % 4;
+          const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], c, -lse2));
+          x[i] = p * (y[i] - delta);
+          if (mask && key >= seen) x[i] = 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const frag_t<T> sf = to_frag<T>(x, 8 * j);
+#pragma unroll
+          for (int d = 0; d < D / 32; ++d) g[d] = mma(L::cols(kt, 32 * n + 16 * j, 32 * d), sf, g[d]);
+        }
+      }
+    }
+    if (t + 1 < t1) {
+      ks.store(lds[(t + 1) & 1][0]);
+      vs.store(lds[(t + 1) & 1][1]);
+    }
+    __syncthreads();
+  }
+  if (r < rows) {
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d) store_col<T>((T*)a.dq + at * a.dim, g[d], 32 * d, a.dim, a.scale);
+  }
+}
+
+// dK and dV: waves of 32 keys over the packed rows that see them.
+//   S = Q K^T, dP = dO V^T, dV^T += dO^T P, dK^T += Q^T dS.
+template <class T, int D, int NW, int BQ>
+__global__ __launch_bounds__(NW * 64) void k_attention_dkv(AttnArgs a) {
+  using L = Tile<T, D, BQ>;
+  constexpr int NT = NW * 64, BK = NW * 32;
+  __shared__ __attribute__((aligned(16))) char lds[2][2][L::kBytes];
+  __shared__ float stat[2][2][BQ];
+  const int kvh = (int)(blockIdx.x % (unsigned)a.kv_heads);
+  const int64_t slot = blockIdx.x / (unsigned)a.kv_heads;
+  int64_t first;
+  const int s = seq_of_slot(a.k_off, a.n_seq, a.n_k, 1, BK, slot, &first);
+  const Seq e = seq_of(a, s);
+  const int64_t j0_64 = (slot - first) * BK;
+  if (j0_64 < 0 || j0_64 >= e.lk) return;
+  const int j0 = (int)j0_64;
+  const int rows = e.lq * a.group;
+  const int w = wave(), l32 = lane() & 31, h = lane() >> 5;
+  const int key = j0 + w * 32 + l32;
+  // First query that sees any key of the tile.
+  int q_first = a.causal ? j0 - (e.lk - e.lq) : 0;
+  q_first = q_first < 0 ? 0 : q_first > e.lq ? e.lq : q_first;
+  const int t0 = q_first * a.group / BQ, t1 = (rows + BQ - 1) / BQ;
+
+  const T* q = (const T*)a.q + e.q0 * a.q_row + (int64_t)kvh * a.group * a.q_head;
+  const int64_t at0 = e.q0 * a.heads + (int64_t)kvh * a.group;
+  const T* k = (const T*)a.k + e.k0 * a.k_row + (int64_t)kvh * a.k_head;
+  const T* v = (const T*)a.v + e.k0 * a.v_row + (int64_t)kvh * a.v_head;
+  frag_t<T> kf[D / 16], vf[D / 16];
+  const bool valid = key < e.lk;
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i) {
+    kf[i] = global_frag<T>(k + (int64_t)(valid ? key : 0) * a.k_row, valid, 16 * i, a.dim);
+    vf[i] = global_frag<T>(v + (int64_t)(valid ? key : 0) * a.v_row, valid, 16 * i, a.dim);
+  }
+  f32x16 gk[D / 32], gv[D / 32];
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d) gk[d] = gv[d] = zero16();
+  const float c = a.scale * kLog2e;
+  constexpr float kUp = (float)(1 << Frag<T>::kShift), kDown = 1.f / kUp;
+
+  Stage<T, D, BQ, NT> qs, ds;
+  float ss = 0.f, sd = 0.f;
+  const auto load = [&](int t) {
+    qs.load(a.dim, [&](int r) { return t * BQ + r < rows ? q + row_offset(a, t * BQ + r, a.q_row, a.q_head) : nullptr; });
+    ds.load(a.dim, [&](int r) {
+      return t * BQ + r < rows ? (const T*)a.dout + (at0 + row_offset(a, t * BQ + r, a.heads, 1)) * a.dim : nullptr;
+    });
+    if (threadIdx.x < BQ) {
+      const int r = t * BQ + (int)threadIdx.x;
+      const int64_t at = at0 + row_offset(a, r < rows ? r : rows - 1, a.heads, 1);
+      ss = r < rows ? a.lse2[at] - (float)Frag<T>::kShift : OC_INF;
+      sd = a.delta[at] * kDown;
+    }
+  };
+  const auto store = [&](int b) {
+    qs.store(lds[b][0]);
+    ds.store(lds[b][1]);
+    if (threadIdx.x < BQ) {
+      stat[b][0][threadIdx.x] = ss;
+      stat[b][1][threadIdx.x] = sd;
+    }
+  };
+  if (t0 < t1) {
+    load(t0);
+    store(0);
+  }
+  __syncthreads();
+  for (int t = t0; t < t1; ++t) {
+    const int b = (t - t0) & 1;
+    const char* qt = lds[b][0];
+    const char* dt = lds[b][1];
+    if (t + 1 < t1) load(t + 1);
+#pragma unroll
+    for (int n = 0; n < BQ / 32; ++n) {
+      f32x16 x = zero16(), y = zero16();
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) x = mma(L::rows(qt, 32 * n, 16 * i), kf[i], x);
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) y = mma(L::rows(dt, 32 * n, 16 * i), vf[i], y);
+      const int rn = t * BQ + 32 * n;
+      // The tile's first row sees the fewest keys.
+      const bool mask = a.causal && seen_keys(a, e, rn) < j0 + w * 32 + 32;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int rr = 8 * (i / 4) + 4 * h + i % 4;
+        float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], c, -stat[b][0][32 * n + rr]));
+        float g = p * __builtin_fmaf(y[i], kDown, -stat[b][1][32 * n + rr]);
+        if (mask && key >= seen_keys(a, e, rn + rr)) p = g = 0.f;
+        x[i] = p;
+        y[i] = g;
+      }
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const frag_t<T> pf = to_frag<T>(x, 8 * j), sf = to_frag<T>(y, 8 * j);
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d) gv[d] = mma(L::cols(dt, 32 * n + 16 * j, 32 * d), pf, gv[d]);
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d) gk[d] = mma(L::cols(qt, 32 * n + 16 * j, 32 * d), sf, gk[d]);
+      }
+    }
+    if (t + 1 < t1) store((t + 1 - t0) & 1);
+    __syncthreads();
+  }
+  if (valid) {
+    const int64_t at = ((e.k0 + key) * a.kv_heads + kvh) * a.dim;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d) {
+      store_col<T>((T*)a.dk + at, gk[d], 32 * d, a.dim, a.scale);
+      store_col<T>((T*)a.dv + at, gv[d], 32 * d, a.dim, kDown);
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Launches
+// ---------------------------------------------------------------------------
+
+template <class F>
+hipError_t by_type(int dtype, F f) {
+  if (dtype == kF32) return f(float());
+  if (dtype == kF16) return f(_Float16());
+  return f(__bf16());
+}
+
+template <int N>
+struct Int {
+  static constexpr int value = N;
+};
+
+template <class F>
+hipError_t by_dim(int dim, F f) {
+  if (dim <= 32) return f(Int<32>());
+  if (dim <= 64) return f(Int<64>());
+  if (dim <= 96) return f(Int<96>());
+  return f(Int<128>());
+}
+
+int64_t slots_of(int64_t rows, int tile, int n_seq) { return rows / tile + n_seq; }
+
+}  // namespace
+
+void attention_set_group(AttnArgs* a) {
+  a->group = a->heads / a->kv_heads;
+  const uint32_t d = (uint32_t)a->group;
+  int l = 0;
+  while ((1u << l) < d) ++l;
+  a->div_shift = l;
+  a->div_mul = (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << l) - d)) / d + 1);
+}
+
+constexpr int kFwdWaves = 4, kFwdTile = kFwdWaves * 32, kFwdKeys = 64;
+
+int attention_splits(int64_t n_q, int64_t n_k, int n_seq, int heads, int kv_heads) {
+  const int group = heads / kv_heads;
+  const int64_t wgs = slots_of(n_q * group, kFwdTile, n_seq) * kv_heads;
+  const int64_t steps = n_k / n_seq / (2 * kFwdKeys);  // parts of two steps at least
+  int64_t n = 512 / wgs;
+  if (n > steps) n = steps;
+  if (n > 64) n = 64;
+  return n < 1 ? 1 : (int)n;
+}
+
+hipError_t launch_attention(const AttnArgs& a, int dtype, hipStream_t s) {
+  const int64_t wgs = slots_of(a.n_q * a.group, kFwdTile, a.n_seq) * a.kv_heads;
+  return by_type(dtype, [&](auto t) {
+    using T = decltype(t);
+    hipError_t err = by_dim(a.dim, [&](auto d) {
+      k_attention<T, decltype(d)::value, 1, kFwdWaves, kFwdKeys>
+          <<<dim3((unsigned)wgs, (unsigned)a.n_split), kFwdWaves * 64, 0, s>>>(a);
+      return hipGetLastError();
+    });
+    if (err != hipSuccess || a.n_split == 1) return err;
+    k_attention_join<T><<<(unsigned)((a.n_q * a.heads + 3) / 4), 256, 0, s>>>(a);
+    return hipGetLastError();
+  });
+}
+
+hipError_t launch_attention_backward(const AttnArgs& a, int dtype, hipStream_t s) {
+  return by_type(dtype, [&](auto t) {
+    using T = decltype(t);
+    if (a.n_q > 0) {
+      k_attention_delta<T><<<(unsigned)((a.n_q * a.heads + 15) / 16), 256, 0, s>>>(a);
+      hipError_t err = hipGetLastError();
+      if (err != hipSuccess) return err;
+    }
+    return by_dim(a.dim, [&](auto d) {
+      constexpr int D = decltype(d)::value;
+      constexpr int B = sizeof(T) == 4 ? 32 : 64;
+      if (a.n_q > 0)
+        k_attention_dq<T, D, 4, B>
+            <<<(unsigned)(slots_of(a.n_q * a.group, 128, a.n_seq) * a.kv_heads), 256, 0, s>>>(a);
+      hipError_t err = hipGetLastError();
+      if (err != hipSuccess) return err;
+      if (a.n_k > 0)
+        k_attention_dkv<T, D, 4, B><<<(unsigned)(slots_of(a.n_k, 128, a.n_seq) * a.kv_heads), 256, 0, s>>>(a);
+      return hipGetLastError();
+    });
+  });
+}
+
+}  // namespace oci

@@ -21,15 +21,19 @@ LIB_PATH = os.path.join(_HERE, "liboctnet_hip.so")
 OC_OK = 0
 OC_SPLIT_MIXED, OC_SPLIT_ANY = 0, 1
 OC_POOL_AVG, OC_POOL_MAX = 0, 1
+OC_F32, OC_F16, OC_BF16 = 0, 1, 2
 OC_CONV_AUTO, OC_CONV_GENERIC, OC_CONV_MFMA, OC_CONV_GEMM, OC_CONV_TRUNCATED = 0, 1, 2, 3, 4
 
 _IMPL = {"auto": OC_CONV_AUTO, "generic": OC_CONV_GENERIC, "mfma": OC_CONV_MFMA, "gemm": OC_CONV_GEMM,
          "truncated": OC_CONV_TRUNCATED}
 
+_TYPES = {torch.float32: OC_F32, torch.float16: OC_F16, torch.bfloat16: OC_BF16}
+
 _P = ctypes.c_void_p
 _I = ctypes.c_int
 _L = ctypes.c_int64
 _S = ctypes.c_size_t
+_F = ctypes.c_float
 
 # name -> (restype, argtypes); mirrors include/octnet_hip.h
 SIGNATURES = {
@@ -73,6 +77,12 @@ SIGNATURES = {
     "oc_points_workspace": (_S, [_L, _I]),
     "oc_points_average": (_I, [_P, _L, _P, _I, _L, _P, _P, _S, _P]),
     "oc_points_vote": (_I, [_P, _L, _P, _I, _L, _P, _P, _S, _P]),
+    "oc_attention_workspace": (_I, [_L, _L, _I, _I, _I, _I, _P]),
+    "oc_attention": (_I, [_P, _L, _L, _P, _L, _L, _P, _L, _L, _P, _P, _P, _I, _L, _L, _I, _I, _I, _I, _F, _I, _P,
+                          _P, _P, _S, _P]),
+    "oc_attention_backward_workspace": (_I, [_L, _L, _I, _I, _I, _I, _P]),
+    "oc_attention_backward": (_I, [_P, _L, _L, _P, _L, _L, _P, _L, _L, _P, _P, _P, _P, _P, _I, _L, _L, _I, _I, _I,
+                                   _I, _F, _I, _P, _P, _P, _P, _S, _P]),
 }
 
 _lib = None
@@ -505,3 +515,104 @@ def points_vote(g: Octree, rows: torch.Tensor, labels: torch.Tensor, n_labels: i
     _check(lib().oc_points_vote(_ptr(rows), rows.shape[0], _ptr(labels), n_labels, g.n_leaves, _ptr(out),
                                 _ptr(ws), ws.numel(), _stream()), "oc_points_vote")
     return out
+
+
+def _type(t: torch.Tensor) -> int:
+    if t.dtype not in _TYPES:
+        raise OctNetError("expected float32, float16 or bfloat16, got %s" % t.dtype)
+    return _TYPES[t.dtype]
+
+
+def leaf_offsets(g: Octree) -> torch.Tensor:
+    """int64 [n + 1]: the leaf rows of sample i are offsets[i] .. offsets[i + 1] - 1."""
+    return g.prefix[::g.gd * g.gh * g.gw].contiguous()
+
+
+def _heads(t: torch.Tensor, what: str):
+    """Pointer and strides of a [rows, heads, dim] tensor that may be a slice."""
+    if not t.is_cuda:
+        raise OctNetError("expected a GPU tensor")
+    if t.dim() != 3:
+        raise OctNetError("%s must be [rows, heads, dim]" % what)
+    if t.numel() and t.shape[2] > 1 and t.stride(2) != 1:
+        raise OctNetError("%s must be contiguous along dim" % what)
+    # The stride of an axis of one place is never used.
+    rows = t.stride(0) if t.shape[0] > 1 else 0
+    heads = t.stride(1) if t.shape[1] > 1 else 0
+    return ctypes.c_void_p(t.data_ptr()), rows, heads
+
+
+def _offsets(t: torch.Tensor | None, n: int, what: str):
+    if t is None:
+        return None
+    if t.dtype != torch.int64 or t.dim() != 1 or t.shape[0] != n:
+        raise OctNetError("%s must be int64 [%d]" % (what, n))
+    return _ptr(t)
+
+
+def _attention_shapes(q, k, v, q_offsets, k_offsets):
+    if q.dim() != 3 or k.dim() != 3 or k.shape != v.shape or q.shape[2] != k.shape[2]:
+        raise OctNetError("q must be [n_q, heads, dim], k and v [n_k, kv_heads, dim]")
+    if k.dtype != q.dtype or v.dtype != q.dtype:
+        raise OctNetError("q, k and v must be of one type")
+    if (q_offsets is None) != (k_offsets is None):
+        raise OctNetError("give both offsets or none")
+    n_seq = 1 if q_offsets is None else q_offsets.shape[0] - 1
+    return n_seq, q.shape[0], k.shape[0], q.shape[1], k.shape[1], q.shape[2]
+
+
+def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_offsets: torch.Tensor | None = None,
+              k_offsets: torch.Tensor | None = None, k_lengths: torch.Tensor | None = None, causal: bool = False,
+              scale: float | None = None, ws: torch.Tensor | None = None, out: torch.Tensor | None = None):
+    """(out [n_q, heads, dim], lse float32 [n_q, heads]) of attention over
+    packed sequences: q [n_q, heads, dim], k and v [n_k, kv_heads, dim] (slices
+    of a larger tensor serve), float32, float16 or bfloat16.  Sequence s has
+    query rows q_offsets[s] .. q_offsets[s + 1] - 1 and key rows likewise
+    (int64, see leaf_offsets; None: one sequence), of which k_lengths[s] hold
+    keys (None: all).  causal: a row sees the keys up to its own place, the
+    last query beside the last key.  scale: 1 / sqrt(dim) by default."""
+    dims = _attention_shapes(q, k, v, q_offsets, k_offsets)
+    n_seq, n_q, n_k, heads, kv_heads, dim = dims
+    if out is None:
+        out = torch.empty((n_q, heads, dim), dtype=q.dtype, device=q.device)
+    elif tuple(out.shape) != (n_q, heads, dim) or out.dtype != q.dtype:
+        raise OctNetError("out must be [n_q, heads, dim] of q's type")
+    lse = torch.empty((n_q, heads), dtype=torch.float32, device=q.device)
+    nb = ctypes.c_size_t(0)
+    _check(lib().oc_attention_workspace(n_q, n_k, n_seq, heads, kv_heads, dim, ctypes.byref(nb)), "oc_attention_workspace")
+    if ws is None and nb.value:
+        ws = torch.empty(nb.value, dtype=torch.uint8, device=q.device)
+    _check(lib().oc_attention(*_heads(q, "q"), *_heads(k, "k"), *_heads(v, "v"),
+                              _offsets(q_offsets, n_seq + 1, "q_offsets"), _offsets(k_offsets, n_seq + 1, "k_offsets"),
+                              _offsets(k_lengths, n_seq, "k_lengths"), n_seq, n_q, n_k, heads, kv_heads, dim, _type(q),
+                              dim ** -0.5 if scale is None else scale, int(bool(causal)), _ptr(out), _ptr(lse), _ptr(ws),
+                              0 if ws is None else ws.numel(), _stream()), "oc_attention")
+    return out, lse
+
+
+def attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, lse: torch.Tensor,
+                       dout: torch.Tensor, q_offsets: torch.Tensor | None = None,
+                       k_offsets: torch.Tensor | None = None, causal: bool = False, scale: float | None = None,
+                       ws: torch.Tensor | None = None):
+    """(dq, dk, dv) of attention() from dout [n_q, heads, dim], with the out
+    and lse that it returned."""
+    n_seq, n_q, n_k, heads, kv_heads, dim = _attention_shapes(q, k, v, q_offsets, k_offsets)
+    for t, what in ((out, "out"), (dout, "dout")):
+        if tuple(t.shape) != (n_q, heads, dim) or t.dtype != q.dtype:
+            raise OctNetError("%s must be [n_q, heads, dim] of q's type" % what)
+    if tuple(lse.shape) != (n_q, heads) or lse.dtype != torch.float32:
+        raise OctNetError("lse must be float32 [n_q, heads]")
+    dq = torch.empty((n_q, heads, dim), dtype=q.dtype, device=q.device)
+    dk = torch.empty((n_k, kv_heads, dim), dtype=q.dtype, device=q.device)
+    dv = torch.empty_like(dk)
+    nb = ctypes.c_size_t(0)
+    _check(lib().oc_attention_backward_workspace(n_q, n_k, n_seq, heads, kv_heads, dim, ctypes.byref(nb)),
+           "oc_attention_backward_workspace")
+    if ws is None:
+        ws = torch.empty(nb.value, dtype=torch.uint8, device=q.device)
+    _check(lib().oc_attention_backward(*_heads(q, "q"), *_heads(k, "k"), *_heads(v, "v"), _ptr(out), _ptr(lse), _ptr(dout),
+                                       _offsets(q_offsets, n_seq + 1, "q_offsets"),
+                                       _offsets(k_offsets, n_seq + 1, "k_offsets"), n_seq, n_q, n_k, heads, kv_heads, dim,
+                                       _type(q), dim ** -0.5 if scale is None else scale, int(bool(causal)), _ptr(dq),
+                                       _ptr(dk), _ptr(dv), _ptr(ws), ws.numel(), _stream()), "oc_attention_backward")
+    return dq, dk, dv

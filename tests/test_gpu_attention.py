@@ -1,0 +1,294 @@
+"""Attention over packed sequences against its definition in 64 bits: outputs,
+gradients, few rows against long keys, empty rows and sequences, slices.
+
+Bars.  u is the unit roundoff of the element type, U32 that of float.  Inputs
+are exact, sums run in float.  With A = sum_j p_j |v_j|:
+  - a score carries at most es = U32 (dim + 8) max_j scale sum_d |q_d k_jd|, a
+    probability relative 2 es + 16 U32 (1 + |lse|) =: ep from its score, its
+    row's statistics and the exponential;
+  - probabilities are rounded to the type for the product (u), products are
+    added up over n keys (n U32), the output is rounded (u):
+    |out - want| <= u |want| + (u + n U32 + ep) A.
+  - gradients: the same terms over the absolute values of their own sums, plus
+    delta = sum dout out with out's own error.
+float16 adds its absolute spacing below 2^-14 (2^-25) per rounded factor, the
+others the end of float's range (2^-126, below which factors come out zero).
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from common import U32, log
+
+pytestmark = pytest.mark.gpu
+
+UNIT = {torch.float32: 2.0 ** -24, torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}
+TINY = {torch.float32: 2.0 ** -126, torch.float16: 2.0 ** -25, torch.bfloat16: 2.0 ** -126}
+TYPES = [torch.float32, torch.float16, torch.bfloat16]
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+
+
+def offsets(lengths):
+    return torch.tensor(np.concatenate([[0], np.cumsum(lengths)]), dtype=torch.int64, device="cuda")
+
+
+def reference(q, k, v, q_off, k_off, k_len, causal, scale, u, tiny, dout=None):
+    """out, lse, (dq, dk, dv) in 64 bits on the CPU, and the bar of each."""
+    q, k, v = (t.cpu().double() for t in (q, k, v))
+    nq, H, D = q.shape
+    K = k.shape[1]
+    G = H // K
+    out, lse, bar_o, bar_l = torch.zeros_like(q), torch.full((nq, H), -math.inf, dtype=torch.float64), torch.zeros_like(q), \
+        torch.zeros((nq, H), dtype=torch.float64)
+    grads = None
+    if dout is not None:
+        do = dout.cpu().double()
+        grads = [torch.zeros_like(t) for t in (q, k, v, q, k, v)]
+    for s in range(len(q_off) - 1):
+        a, b, c = q_off[s], q_off[s + 1], k_off[s]
+        m, n = b - a, (k_off[s + 1] - c if k_len is None else k_len[s])
+        if m == 0 or n == 0:
+            continue
+        see = torch.ones(m, n, dtype=torch.bool)
+        if causal:
+            see = torch.arange(n)[None] <= torch.arange(m)[:, None] + (n - m)
+        for h in range(H):
+            Q, Kh, V = q[a:b, h], k[c:c + n, h // G], v[c:c + n, h // G]
+            x = (Q @ Kh.T * scale).masked_fill(~see, -math.inf)
+            mag = (Q.abs() @ Kh.abs().T * scale).masked_fill(~see, 0.0)
+            L = torch.logsumexp(x, 1)
+            L0 = torch.where(L == -math.inf, torch.zeros_like(L), L)
+            P = torch.exp(x - L0[:, None])
+            es = U32 * (D + 8) * mag.amax(1, keepdim=True)
+            ep = 2 * es + 16 * U32 * (1 + L0.abs()[:, None])
+            out[a:b, h], lse[a:b, h] = P @ V, L
+            A = P @ V.abs()
+            bar_o[a:b, h] = u * out[a:b, h].abs() + (u + n * U32 + ep) * A + tiny * (1 + V.abs().sum(0))
+            bar_l[a:b, h] = (es + n * U32)[:, 0] + 8 * U32 * (1 + L0.abs())
+            if dout is None:
+                continue
+            d = do[a:b, h]
+            dP = d @ V.T
+            delta = (d * out[a:b, h]).sum(1, keepdim=True)
+            dS = P * (dP - delta)
+            off = (d.abs() * bar_o[a:b, h]).sum(1, keepdim=True) + D * U32 * (d * out[a:b, h]).abs().sum(1, keepdim=True) \
+                + D * U32 * (d.abs() @ V.abs().T)
+            eS = (u + (m * G + n) * U32 + 2 * ep) * dS.abs() + P * off + tiny
+            eP = (u + m * G * U32 + 2 * ep) * P + tiny
+            g = h // G
+            grads[0][a:b, h] += scale * dS @ Kh
+            grads[1][c:c + n, g] += scale * dS.T @ Q
+            grads[2][c:c + n, g] += P.T @ d
+            grads[3][a:b, h] += scale * eS @ Kh.abs()
+            grads[4][c:c + n, g] += scale * eS.T @ Q.abs()
+            grads[5][c:c + n, g] += eP.T @ d.abs()
+    if grads:
+        for i in range(3):
+            grads[3 + i] += u * grads[i].abs() + tiny
+    return out, lse, bar_o, bar_l, grads
+
+
+def near(got, want, bar, what):
+    got = got.cpu().double()
+    fin = torch.isfinite(want)
+    assert torch.equal(torch.isfinite(got), fin) and torch.equal(got[~fin], want[~fin]), what + ": infinities"
+    err, bar = (got - want)[fin].abs(), bar[fin]
+    if not err.numel():
+        return
+    r = float((err / bar.clamp(min=1e-300)).masked_fill(err == 0, 0.0).max())
+    log("  %s: %.3g of the bar, largest error %.3g" % (what, r, float(err.max())))
+    assert r <= 1.0, what
+
+
+def inputs(seed, dtype, nq, nk, H, K, D, spread=1.5):
+    g = torch.Generator().manual_seed(seed)
+    q = (spread * torch.randn(nq, H, D, generator=g)).to(dtype)
+    k, v, d = (torch.randn(n, h, D, generator=g).to(dtype) for n, h in ((nk, K), (nk, K), (nq, H)))
+    return [t.cuda() for t in (q, k, v, d)]
+
+
+def check(dtype, ql, kl, H, K, D, causal, seed=0, scale=None, backward=True):
+    from paper_1611_05009_amd import octnet as oc
+    q, k, v, d = inputs(seed, dtype, sum(ql), sum(kl), H, K, D)
+    qo, ko = offsets(ql), offsets(kl)
+    kw = dict(q_offsets=qo, k_offsets=ko, causal=causal, scale=scale)
+    out, lse = oc.attention(q, k, v, **kw)
+    grads = oc.attention_backward(q, k, v, out, lse, d, **kw) if backward else None
+    torch.cuda.synchronize()
+    w = reference(q, k, v, qo.tolist(), ko.tolist(), None, causal, scale or D ** -0.5, UNIT[dtype], TINY[dtype],
+                  d if backward else None)
+    near(out, w[0], w[2], "out")
+    near(lse, w[1], w[3], "lse")
+    for i, name in enumerate(("dq", "dk", "dv")):
+        if backward:
+            near(grads[i], w[4][i], w[4][3 + i], name)
+
+
+CASES = [
+    # queries, keys, heads, key heads, dim, causal
+    ([1], [1], 1, 1, 8, True),
+    ([37], [37], 2, 2, 16, False),
+    ([200], [200], 3, 1, 24, True),
+    ([64, 0, 1, 131], [64, 0, 1, 131], 4, 2, 32, True),
+    ([5, 70], [129, 70], 4, 4, 40, True),
+    ([100, 33], [20, 0], 2, 1, 64, True),           # rows that see nothing, no keys at all
+    ([100, 0], [20, 77], 2, 1, 64, False),          # keys that no row sees
+    ([257], [255], 5, 1, 72, False),
+    ([300, 129], [300, 129], 6, 2, 96, True),
+    ([77], [400], 8, 2, 104, True),
+    ([130, 7, 260], [130, 7, 260], 4, 1, 128, True),
+    ([385], [385], 2, 2, 128, False),
+]
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("case", CASES, ids=lambda c: "q%s_k%s_%dof%d_d%d_%s" % (
+    "-".join(map(str, c[0])), "-".join(map(str, c[1])), c[2], c[3], c[4], "causal" if c[5] else "all"))
+def test_attention_and_gradients(dtype, case):
+    check(dtype, *case)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+def test_many_short_sequences(dtype):
+    rng = np.random.default_rng(3)
+    ql = rng.integers(0, 9, size=300).tolist()
+    kl = [n + int(rng.integers(0, 3)) for n in ql]
+    check(dtype, ql, kl, 4, 2, 32, True, seed=4)
+
+
+@pytest.mark.parametrize("scale", [0.5, 3.0])
+def test_steep_scores(scale):
+    """Scores of hundreds: the running maximum moves by far more than a step's
+    rescaling threshold, and most probabilities vanish."""
+    check(torch.bfloat16, [150], [333], 2, 1, 64, False, seed=5, scale=scale)
+    check(torch.float32, [150], [333], 2, 1, 64, True, seed=5, scale=scale)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("rows,keys,heads,kv,dim", [(1, 5000, 8, 1, 128), (1, 2047, 4, 4, 64), (3, 4099, 6, 2, 80),
+                                                   (40, 3001, 2, 1, 32)])
+def test_few_rows_split_keys(dtype, rows, keys, heads, kv, dim):
+    """A part-filled cache with other values (here NaN) behind the keys."""
+    from paper_1611_05009_amd import octnet as oc
+    lens = [keys, 1, 0, keys // 3]
+    q, k, v, _ = inputs(7, dtype, rows * len(lens), keys * len(lens), heads, kv, dim)
+    for i, n in enumerate(lens):
+        k[i * keys + n:(i + 1) * keys] = math.nan
+        v[i * keys + n:(i + 1) * keys] = math.nan
+    qo, ko = offsets([rows] * len(lens)), offsets([keys] * len(lens))
+    kl = torch.tensor(lens, dtype=torch.int64, device="cuda")
+    for causal in (True, False):
+        out, lse = oc.attention(q, k, v, q_offsets=qo, k_offsets=ko, k_lengths=kl, causal=causal)
+        torch.cuda.synchronize()
+        w = reference(q, k, v, qo.tolist(), ko.tolist(), lens, causal, dim ** -0.5, UNIT[dtype], TINY[dtype])
+        near(out, w[0], w[2] + 4 * U32 * w[0].abs(), "out")
+        near(lse, w[1], w[3] + 8 * U32, "lse")
+
+
+def test_slices_and_one_sequence():
+    """Queries, keys and values as slices of one projection's output, no
+    offsets; the same bits as from contiguous copies."""
+    from paper_1611_05009_amd import octnet as oc
+    x = torch.randn(391, 8, 64, generator=torch.Generator().manual_seed(1)).to(torch.bfloat16).cuda()
+    q, k, v = x[:, :4], x[:, 4:6], x[:, 6:]
+    a, la = oc.attention(q, k, v, causal=True)
+    one = offsets([391])
+    b, lb = oc.attention(q.contiguous(), k.contiguous(), v.contiguous(), q_offsets=one, k_offsets=one, causal=True)
+    assert torch.equal(a, b) and torch.equal(la, lb)
+    d = torch.randn_like(a)
+    for s, t in zip(oc.attention_backward(q, k, v, a, la, d, causal=True),
+                    oc.attention_backward(q.contiguous(), k.contiguous(), v.contiguous(), b, lb, d, q_offsets=one,
+                                          k_offsets=one, causal=True)):
+        assert torch.equal(s, t)
+    # head-major storage
+    y = x.transpose(0, 1).contiguous().transpose(0, 1)
+    c, _ = oc.attention(y[:, :4], y[:, 4:6], y[:, 6:], causal=True)
+    assert torch.equal(a, c)
+
+
+def test_outside_rows_do_not_matter():
+    """NaN beside a sequence's rows (the next sequence's, and those of no
+    sequence) and in later keys of a causal sequence's own scores."""
+    from paper_1611_05009_amd import octnet as oc
+    for dtype in TYPES:
+        q, k, v, d = inputs(11, dtype, 300, 300, 2, 2, 40)
+        for t in (q, k, v):
+            t[100:170] = math.nan
+            t[270:] = math.nan
+        off = torch.tensor([0, 100, 170, 270], dtype=torch.int64, device="cuda")
+        out, lse = oc.attention(q, k, v, q_offsets=off, k_offsets=off)
+        keep = torch.cat([torch.arange(100), torch.arange(170, 270)]).cuda()
+        o2 = offsets([100, 100])
+        want, wl = oc.attention(q[keep], k[keep], v[keep], q_offsets=o2, k_offsets=o2)
+        assert torch.equal(out[keep], want) and torch.equal(lse[keep], wl)
+
+
+def test_results_do_not_vary():
+    from paper_1611_05009_amd import octnet as oc
+    q, k, v, d = inputs(13, torch.bfloat16, 700, 700, 8, 2, 128)
+    off = offsets([260, 440])
+    kw = dict(q_offsets=off, k_offsets=off, causal=True)
+    first = None
+    for _ in range(3):
+        out, lse = oc.attention(q, k, v, **kw)
+        r = (out, lse) + oc.attention_backward(q, k, v, out, lse, d, **kw)
+        first = first or r
+        assert all(torch.equal(a, b) for a, b in zip(first, r))
+
+
+@pytest.mark.parametrize("causal", [False, True])
+def test_gradients_against_differences(causal):
+    """Central differences of the 64-bit loss sum(out dout) along a random
+    direction of (q, k, v) against the gradients' product with it.  The
+    difference's own error is of order t^2 = 1e-8 of the third derivative,
+    the gradients' that of float (their bar sums to below 1e-4 here)."""
+    from paper_1611_05009_amd import octnet as oc
+    ql, kl, H, K, D = [33, 21], [33, 40], 4, 2, 16
+    q, k, v, d = inputs(17, torch.float32, sum(ql), sum(kl), H, K, D, spread=1.0)
+    kw = dict(q_offsets=offsets(ql), k_offsets=offsets(kl), causal=causal)
+    out, lse = oc.attention(q, k, v, **kw)
+    grads = oc.attention_backward(q, k, v, out, lse, d, **kw)
+    g = torch.Generator().manual_seed(18)
+    dirs = [torch.randn(t.shape, generator=g, dtype=torch.float64) for t in (q, k, v)]
+    t = 1e-4
+
+    def loss(sign):
+        w = reference(*[x.cpu().double() + sign * t * y for x, y in zip((q, k, v), dirs)], kw["q_offsets"].tolist(),
+                      kw["k_offsets"].tolist(), None, causal, D ** -0.5, 0.0, 0.0)
+        return float((w[0] * d.cpu().double()).sum())
+
+    want = (loss(1) - loss(-1)) / (2 * t)
+    got = sum(float((x.cpu().double() * y).sum()) for x, y in zip(grads, dirs))
+    size = sum(float((x.cpu().double() * y).abs().sum()) for x, y in zip(grads, dirs))
+    log("  difference %.8g, product %.8g" % (want, got))
+    assert abs(got - want) <= 1e-4 + 1e-6 * size
+
+
+def test_long_cache_past_32_bits():
+    """Keys whose offsets pass 2^32 bytes and 2^31 elements: one head of a
+    wide cache, the sequence at its end."""
+    from paper_1611_05009_amd import octnet as oc
+    heads, dim, n = 64, 128, 300000     # 2.46e9 elements, 4.9 GB
+    k = torch.zeros((n, heads, dim), dtype=torch.float16, device="cuda")
+    v = torch.zeros_like(k)
+    tail = 1000
+    g = torch.Generator().manual_seed(2)
+    kt, vt = (torch.randn(tail, heads, dim, generator=g).half() for _ in range(2))
+    k[n - tail:], v[n - tail:] = kt.cuda(), vt.cuda()
+    q = torch.randn(2, heads, dim, generator=g).half().cuda()
+    qo = torch.tensor([0, 1, 2], dtype=torch.int64, device="cuda")
+    ko = torch.tensor([0, n - tail, n], dtype=torch.int64, device="cuda")
+    out, lse = oc.attention(q, k, v, q_offsets=qo, k_offsets=ko)
+    o1 = offsets([1])
+    o2 = offsets([tail])
+    w = reference(q[1:], kt, vt, o1.tolist(), o2.tolist(), None, False, dim ** -0.5, UNIT[torch.float16], TINY[torch.float16])
+    near(out[1:], w[0], w[2] + 4 * U32 * w[0].abs(), "out")
+    near(lse[1:], w[1], w[3] + 8 * U32, "lse")
+    assert not out[0].any() and torch.allclose(lse[0], torch.full_like(lse[0], math.log(n - tail)), rtol=1e-5)
