@@ -75,6 +75,7 @@ extern "C" {
 #define OC_F32 0
 #define OC_F16 1
 #define OC_BF16 2
+#define OC_F8 3 /* output only: 4 bits of exponent, 3 of mantissa, no infinity, up to 448 */
 
 /*
  * Header-only helpers on one shallow octree's bit string t[4] (layout
@@ -532,6 +533,78 @@ int oc_attention_backward(const void* q, int64_t q_row, int64_t q_head, const vo
                           int n_seq, int64_t n_q, int64_t n_k, int heads, int kv_heads, int dim, int dtype,
                           float scale, int causal, void* dq, void* dk, void* dv, void* ws, size_t ws_bytes,
                           void* stream);
+
+/*
+ * Root-mean-square norm of rows, the residual added first:
+ *   sum = x + residual,  y = sum / sqrt(mean(sum^2) + eps) * weight,
+ * both from the unrounded sum.
+ *   x: [rows][c] of type x_type; residual, sum: [rows][c] of type sum_type
+ *   (x_type or OC_F32), either may be NULL (no residual; sum not written);
+ *   weight: float [c]; 1 <= c <= 32768.
+ *   y: [rows][c] of type y_type: x_type; any type where x is OC_F32; or
+ *   OC_F8, where a row holds y / scale[row], rounded to nearest, with
+ *   scale[row] = max |y| / 448 (1 for a row of zeros).  scale: float [rows],
+ *   used with OC_F8 only.
+ * sum may be the residual itself (in place); other outputs alias no input.
+ */
+int oc_rms_norm(const void* x, int x_type, const void* residual, int sum_type, const float* weight, int64_t rows,
+                int c, float eps, void* sum, void* y, int y_type, float* scale, void* stream);
+
+/* Gradients of oc_rms_norm (y not in 8 bits), from the sum that it wrote (of
+ * type sum_type; x where there was no residual), dy (y_type) and dsum
+ * (sum_type, NULL: zero), the gradient that reaches sum by other ways:
+ *   dx = dsum + the gradient through y, [rows][c] of sum_type, which is x's
+ *   and the residual's alike; dweight: float [c] (NULL: not wanted).
+ * The rows' terms of dweight are added up in a fixed order. */
+int oc_rms_norm_backward_workspace(int64_t rows, int c, size_t* bytes);
+int oc_rms_norm_backward(const void* sum, int sum_type, const float* weight, const void* dy, int y_type,
+                         const void* dsum, int64_t rows, int c, float eps, void* dx, float* dweight, void* ws,
+                         size_t ws_bytes, void* stream);
+
+/*
+ * Log probabilities of given labels, with entropy and the top alternatives:
+ *   lse = log sum_j exp(logits[row][j]),
+ *   logprob = logits[row][label] - lse (0 where the label is outside
+ *   [0, classes): an unlabelled row, as oc_points_vote leaves them at -1),
+ *   entropy = -sum_j p_j log p_j,
+ *   top_logprob, top_label [rows][top]: the `top` greatest, in descending
+ *   order, equal ones in the order of their indices.
+ * A logit of -infinity rules its class out.  A row without any class left has
+ * lse = logprob = -inf and entropy 0, and its top labels are 0, 1, ...  A NaN
+ * shows in lse, logprob and entropy and is no alternative (label -1, NaN,
+ * where fewer than `top` numbers are left).
+ *   logits: [rows][classes] of type dtype, labels: int32 [rows]; 0 <= top <=
+ *   min(classes, 32); logprob, lse: float [rows]; entropy: float [rows], or
+ *   NULL (not wanted).
+ */
+int oc_label_logprobs_workspace(int64_t rows, int classes, int top, size_t* bytes);
+int oc_label_logprobs(const void* logits, int dtype, const int32_t* labels, int64_t rows, int classes, int top,
+                      float* logprob, float* lse, float* entropy, float* top_logprob, int32_t* top_label, void* ws,
+                      size_t ws_bytes, void* stream);
+
+/* Gradient of oc_label_logprobs with respect to the logits, from its lse (and
+ * entropy, where dentropy is given):
+ *   dlogits[j] = dlogprob ([j = label] - p_j) - dentropy p_j (log p_j + entropy),
+ * of type dtype; dlogprob, dentropy: float [rows], either may be NULL (zero).
+ * Unlabelled rows take no part in dlogprob, rows without a class in either.
+ * dlogits may be the logits themselves (in place). */
+int oc_label_logprobs_backward(const void* logits, int dtype, const int32_t* labels, int64_t rows, int classes,
+                               const float* lse, const float* dlogprob, const float* entropy,
+                               const float* dentropy, void* dlogits, void* stream);
+
+/*
+ * Global norm of n gradient tensors, and their clipping:
+ *   norm = sqrt(sum of squares over all tensors),
+ *   out[i] = grads[i] * min(1, max_norm / (norm + 1e-6)).
+ * grads, out, counts, dtypes are arrays of length n on the host [host] (device
+ * pointers, element counts, OC_F32 / OC_F16 / OC_BF16); out[i] may be grads[i]
+ * (in place, nothing is then written where the factor is 1).  A count of 0 is
+ * skipped.  norm: float, on the device.  The squares are added up in double,
+ * in a fixed order.  A norm that is infinite or NaN makes the factor 0 or NaN.
+ */
+int oc_clip_grad_norm_workspace(const int64_t* counts, int n, size_t* bytes);
+int oc_clip_grad_norm(const void* const* grads, void* const* out, const int64_t* counts, const int* dtypes, int n,
+                      float max_norm, float* norm, void* ws, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

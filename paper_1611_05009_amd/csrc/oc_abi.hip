@@ -776,4 +776,251 @@ int oc_attention_backward(const void* q, int64_t q_row, int64_t q_head, const vo
   return OC_OK;
 }
 
+namespace {
+
+int norm_sizes(const char* who, int64_t rows, int c) {
+  if (rows < 0 || c <= 0 || c > oci::kNormMaxWidth)
+    return fail(OC_EINVAL, "%s: %lld rows of width %d (1 to %d)", who, (long long)rows, c, oci::kNormMaxWidth);
+  if (rows > (1LL << 62) / c / 8) return fail(OC_EOVERFLOW, "%s: too many rows", who);
+  return OC_OK;
+}
+
+}  // namespace
+
+int oc_rms_norm(const void* x, int x_type, const void* residual, int sum_type, const float* weight, int64_t rows,
+                int c, float eps, void* sum, void* y, int y_type, float* scale, void* stream) {
+  g_last_error.clear();
+  const int rc = norm_sizes("oc_rms_norm", rows, c);
+  if (rc != OC_OK) return rc;
+  if (!type_ok(x_type) || (sum_type != x_type && sum_type != OC_F32))
+    return fail(OC_EINVAL, "oc_rms_norm: bad types %d, %d", x_type, sum_type);
+  if (y_type != x_type && y_type != OC_F8 && !(x_type == OC_F32 && type_ok(y_type)))
+    return fail(OC_EINVAL, "oc_rms_norm: output type %d for input type %d", y_type, x_type);
+  if (!(eps >= 0.f)) return fail(OC_EINVAL, "oc_rms_norm: eps %g is negative", eps);
+  if (rows == 0) return OC_OK;
+  if (!x || !weight || !y || (y_type == OC_F8 && !scale)) return fail(OC_EINVAL, "oc_rms_norm: null pointer");
+  oci::NormArgs a = oci::NormArgs();
+  a.x = x; a.residual = residual; a.weight = weight;
+  a.rows = rows; a.c = c; a.eps = eps;
+  a.sum = sum; a.y = y; a.scale = scale;
+  OC_CHECK_HIP(oci::launch_rms_norm(a, x_type, sum_type, y_type, as_stream(stream)), "oc_rms_norm");
+  return OC_OK;
+}
+
+int oc_rms_norm_backward_workspace(int64_t rows, int c, size_t* bytes) {
+  g_last_error.clear();
+  if (!bytes) return fail(OC_EINVAL, "oc_rms_norm_backward_workspace: null pointer");
+  const int rc = norm_sizes("oc_rms_norm_backward_workspace", rows, c);
+  if (rc != OC_OK) return rc;
+  *bytes = oci::align256(4 * (size_t)oci::norm_back_groups(rows, c) * c);
+  return OC_OK;
+}
+
+int oc_rms_norm_backward(const void* sum, int sum_type, const float* weight, const void* dy, int y_type,
+                         const void* dsum, int64_t rows, int c, float eps, void* dx, float* dweight, void* ws,
+                         size_t ws_bytes, void* stream) {
+  g_last_error.clear();
+  const int rc = norm_sizes("oc_rms_norm_backward", rows, c);
+  if (rc != OC_OK) return rc;
+  if (!type_ok(sum_type) || !type_ok(y_type) || (sum_type != y_type && sum_type != OC_F32))
+    return fail(OC_EINVAL, "oc_rms_norm_backward: bad types %d, %d", sum_type, y_type);
+  if (!(eps >= 0.f)) return fail(OC_EINVAL, "oc_rms_norm_backward: eps %g is negative", eps);
+  if (!weight || (rows > 0 && (!sum || !dy || !dx))) return fail(OC_EINVAL, "oc_rms_norm_backward: null pointer");
+  if (rows == 0 && !dweight) return OC_OK;
+  const size_t need = 4 * (size_t)oci::norm_back_groups(rows, c) * c;
+  if (dweight && need && (!ws || ws_bytes < need)) return fail(OC_EWORKSPACE, "oc_rms_norm_backward: workspace too small");
+  oci::NormArgs a = oci::NormArgs();
+  a.weight = weight;
+  a.rows = rows; a.c = c; a.eps = eps;
+  a.sum = const_cast<void*>(sum); a.dy = dy; a.dsum = dsum; a.dx = dx;
+  a.part = dweight ? static_cast<float*>(ws) : nullptr;
+  OC_CHECK_HIP(oci::launch_rms_norm_back(a, sum_type, y_type, dweight, as_stream(stream)), "oc_rms_norm_backward");
+  return OC_OK;
+}
+
+namespace {
+
+int label_sizes(const char* who, int64_t rows, int classes, int top) {
+  if (rows < 0 || classes <= 0) return fail(OC_EINVAL, "%s: %lld rows of %d classes", who, (long long)rows, classes);
+  if (top < 0 || top > oci::kMostTop || top > classes)
+    return fail(OC_EINVAL, "%s: top %d of %d classes (at most %d)", who, top, classes, oci::kMostTop);
+  if (rows >= (1LL << 31)) return fail(OC_EOVERFLOW, "%s: rows >= 2^31", who);
+  if (classes > (1 << 29)) return fail(OC_EOVERFLOW, "%s: classes > 2^29", who);
+  return OC_OK;
+}
+
+// Offsets of the parts of long rows in the workspace: statistics, values,
+// indices, end.
+void label_parts_at(int64_t rows, int classes, int top, size_t at[4]) {
+  const int parts = oci::label_parts(rows, classes);
+  const size_t n = parts > 1 ? (size_t)rows * parts : 0;
+  at[0] = 0;
+  at[1] = oci::align256(12 * n);
+  at[2] = at[1] + oci::align256(4 * n * top);
+  at[3] = at[2] + oci::align256(4 * n * top);
+}
+
+}  // namespace
+
+int oc_label_logprobs_workspace(int64_t rows, int classes, int top, size_t* bytes) {
+  g_last_error.clear();
+  if (!bytes) return fail(OC_EINVAL, "oc_label_logprobs_workspace: null pointer");
+  const int rc = label_sizes("oc_label_logprobs_workspace", rows, classes, top);
+  if (rc != OC_OK) return rc;
+  size_t at[4];
+  label_parts_at(rows, classes, top, at);
+  *bytes = at[3];
+  return OC_OK;
+}
+
+int oc_label_logprobs(const void* logits, int dtype, const int32_t* labels, int64_t rows, int classes, int top,
+                      float* logprob, float* lse, float* entropy, float* top_logprob, int32_t* top_label, void* ws,
+                      size_t ws_bytes, void* stream) {
+  g_last_error.clear();
+  const int rc = label_sizes("oc_label_logprobs", rows, classes, top);
+  if (rc != OC_OK) return rc;
+  if (!type_ok(dtype)) return fail(OC_EINVAL, "oc_label_logprobs: bad type %d", dtype);
+  if (rows == 0) return OC_OK;
+  if (!logits || !labels || !logprob || !lse || (top && (!top_logprob || !top_label)))
+    return fail(OC_EINVAL, "oc_label_logprobs: null pointer");
+  size_t at[4];
+  label_parts_at(rows, classes, top, at);
+  if (at[3] && (!ws || ws_bytes < at[3])) return fail(OC_EWORKSPACE, "oc_label_logprobs: workspace too small");
+  if (!aligned16(ws)) return fail(OC_EINVAL, "oc_label_logprobs: workspace not aligned to 16 bytes");
+  oci::LabelArgs a = oci::LabelArgs();
+  a.logits = logits; a.labels = labels;
+  a.rows = rows; a.classes = classes; a.top = top;
+  a.logprob = logprob; a.lse = lse; a.entropy = entropy;
+  a.top_logprob = top_logprob; a.top_label = top_label;
+  a.part_stat = static_cast<float*>(ws);
+  a.part_val = reinterpret_cast<float*>(static_cast<char*>(ws) + at[1]);
+  a.part_idx = reinterpret_cast<int*>(static_cast<char*>(ws) + at[2]);
+  OC_CHECK_HIP(oci::launch_labels(a, dtype, as_stream(stream)), "oc_label_logprobs");
+  return OC_OK;
+}
+
+int oc_label_logprobs_backward(const void* logits, int dtype, const int32_t* labels, int64_t rows, int classes,
+                               const float* lse, const float* dlogprob, const float* entropy,
+                               const float* dentropy, void* dlogits, void* stream) {
+  g_last_error.clear();
+  const int rc = label_sizes("oc_label_logprobs_backward", rows, classes, 0);
+  if (rc != OC_OK) return rc;
+  if (!type_ok(dtype)) return fail(OC_EINVAL, "oc_label_logprobs_backward: bad type %d", dtype);
+  if (rows == 0) return OC_OK;
+  if (!logits || !labels || !lse || !dlogits || (dentropy && !entropy))
+    return fail(OC_EINVAL, "oc_label_logprobs_backward: null pointer");
+  oci::LabelArgs a = oci::LabelArgs();
+  a.logits = logits; a.labels = labels;
+  a.rows = rows; a.classes = classes;
+  a.lse = const_cast<float*>(lse); a.entropy = const_cast<float*>(entropy);
+  a.dlogprob = dlogprob; a.dentropy = dentropy; a.dlogits = dlogits;
+  OC_CHECK_HIP(oci::launch_labels_back(a, dtype, as_stream(stream)), "oc_label_logprobs_backward");
+  return OC_OK;
+}
+
+}  // extern "C"
+
+namespace {
+
+int64_t clip_chunks(int64_t count) { return (count + oci::kClipChunk - 1) / oci::kClipChunk; }
+
+// Walks the tensors in batches of one launch: f(batch, workgroups, first partial sum).
+template <class F>
+int each_clip_batch(const void* const* grads, void* const* out, const int64_t* counts, const int* dtypes, int n, F f) {
+  int64_t parts = 0;
+  for (int i = 0; i < n;) {
+    oci::ClipBatch b;
+    b.n = 0;
+    b.first[0] = 0;
+    int64_t chunks = 0;
+    for (; i < n && b.n < oci::kClipBatch; ++i) {
+      if (counts[i] == 0) continue;
+      const int64_t more = clip_chunks(counts[i]);
+      if (chunks + more > 0x7fffffff) break;
+      b.in[b.n] = grads ? grads[i] : nullptr;
+      b.out[b.n] = out ? out[i] : nullptr;
+      b.count[b.n] = counts[i];
+      b.type[b.n] = dtypes ? (uint8_t)dtypes[i] : 0;
+      chunks += more;
+      b.first[++b.n] = (uint32_t)chunks;
+    }
+    const int groups = (int)(chunks < oci::kClipParts ? chunks : oci::kClipParts);
+    const int rc = f(b, groups, parts);
+    if (rc != OC_OK) return rc;
+    parts += groups;
+  }
+  return OC_OK;
+}
+
+int clip_counts(const char* who, const int64_t* counts, int n) {
+  if (n < 0 || (n > 0 && !counts)) return fail(OC_EINVAL, "%s: null pointer or negative count of tensors", who);
+  for (int i = 0; i < n; ++i) {
+    if (counts[i] < 0) return fail(OC_EINVAL, "%s: tensor %d has %lld elements", who, i, (long long)counts[i]);
+    if (clip_chunks(counts[i]) > 0x7fffffff) return fail(OC_EOVERFLOW, "%s: tensor %d too large", who, i);
+  }
+  return OC_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int oc_clip_grad_norm_workspace(const int64_t* counts, int n, size_t* bytes) {
+  g_last_error.clear();
+  if (!bytes) return fail(OC_EINVAL, "oc_clip_grad_norm_workspace: null pointer");
+  const int rc = clip_counts("oc_clip_grad_norm_workspace", counts, n);
+  if (rc != OC_OK) return rc;
+  int64_t parts = 0;
+  each_clip_batch(nullptr, nullptr, counts, nullptr, n, [&](const oci::ClipBatch&, int groups, int64_t) {
+    parts += groups;
+    return OC_OK;
+  });
+  *bytes = oci::align256(8 * (size_t)parts + 8);
+  return OC_OK;
+}
+
+int oc_clip_grad_norm(const void* const* grads, void* const* out, const int64_t* counts, const int* dtypes, int n,
+                      float max_norm, float* norm, void* ws, size_t ws_bytes, void* stream) {
+  g_last_error.clear();
+  const int rc = clip_counts("oc_clip_grad_norm", counts, n);
+  if (rc != OC_OK) return rc;
+  if (!norm || (n > 0 && (!grads || !out || !dtypes))) return fail(OC_EINVAL, "oc_clip_grad_norm: null pointer");
+  if (!(max_norm >= 0.f)) return fail(OC_EINVAL, "oc_clip_grad_norm: max_norm %g is negative", max_norm);
+  for (int i = 0; i < n; ++i) {
+    if (!type_ok(dtypes[i])) return fail(OC_EINVAL, "oc_clip_grad_norm: tensor %d has a bad type %d", i, dtypes[i]);
+    if (counts[i] > 0 && (!grads[i] || !out[i])) return fail(OC_EINVAL, "oc_clip_grad_norm: tensor %d is null", i);
+    const uintptr_t step = (uintptr_t)type_bytes(dtypes[i]) - 1;
+    if (((uintptr_t)grads[i] | (uintptr_t)out[i]) & step)
+      return fail(OC_EINVAL, "oc_clip_grad_norm: tensor %d is not aligned to its elements", i);
+  }
+  size_t need = 0;
+  oc_clip_grad_norm_workspace(counts, n, &need);
+  if (!ws || ws_bytes < need) return fail(OC_EWORKSPACE, "oc_clip_grad_norm: workspace too small");
+  if ((uintptr_t)ws & 7) return fail(OC_EINVAL, "oc_clip_grad_norm: workspace not aligned to 8 bytes");
+  hipStream_t s = as_stream(stream);
+  double* parts = static_cast<double*>(ws);
+  int64_t total = 0;
+  int done = each_clip_batch(grads, out, counts, dtypes, n, [&](const oci::ClipBatch& b, int groups, int64_t at) {
+    total = at + groups;
+    if (groups == 0) return OC_OK;
+    OC_CHECK_HIP(oci::launch_square_sums(b, parts + at, groups, s), "oc_clip_grad_norm");
+    return OC_OK;
+  });
+  if (done != OC_OK) return done;
+  bool any = false;
+  done = each_clip_batch(grads, out, counts, dtypes, n, [&](const oci::ClipBatch& b, int groups, int64_t) {
+    if (groups == 0) return OC_OK;
+    any = true;
+    OC_CHECK_HIP(oci::launch_clip(b, parts, (int)total, max_norm, norm, groups, s), "oc_clip_grad_norm");
+    return OC_OK;
+  });
+  if (done != OC_OK || any) return done;
+  // No element at all: the norm of nothing.
+  oci::ClipBatch none;
+  none.n = 0;
+  none.first[0] = 0;
+  OC_CHECK_HIP(oci::launch_clip(none, parts, 0, max_norm, norm, 1, s), "oc_clip_grad_norm");
+  return OC_OK;
+}
+
 }  // extern "C"

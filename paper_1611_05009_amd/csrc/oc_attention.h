@@ -1,11 +1,8 @@
 // Arguments of the attention kernels, shared with the C entry points.
 #pragma once
-#include "oc_internal.h"
+#include "oc_sequence.h"
 
 namespace oci {
-
-// Element types of the sequence operators (the header's OC_F32 ... values).
-constexpr int kF32 = 0, kF16 = 1, kBF16 = 2;
 
 struct AttnArgs {
   const void *q, *k, *v;                 // [n_q][heads][dim], [n_k][kv_heads][dim] by strides

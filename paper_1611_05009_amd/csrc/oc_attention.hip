@@ -737,13 +737,6 @@ __global__ __launch_bounds__(NW * 64) void k_attention_dkv(AttnArgs a) {
 // Launches
 // ---------------------------------------------------------------------------
 
-template <class F>
-hipError_t by_type(int dtype, F f) {
-  if (dtype == kF32) return f(float());
-  if (dtype == kF16) return f(_Float16());
-  return f(__bf16());
-}
-
 template <int N>
 struct Int {
   static constexpr int value = N;

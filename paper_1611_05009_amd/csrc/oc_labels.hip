@@ -1,0 +1,583 @@
+// Log probabilities of labels, with entropy and the top alternatives, and
+// their gradient.
+//
+//   lse = log sum_j exp(x_j),  logprob = x_label - lse,
+//   entropy = -sum_j p_j log p_j = log s - t / s,
+//     s = sum_j exp(x_j - m), t = sum_j exp(x_j - m) (x_j - m), m = max_j x_j;
+//   dx_j = g ([j = label] - p_j) - ge p_j (log p_j + entropy).
+//
+// Memory bound: the logits are read once (the gradient reads them once more
+// and writes as much).  Up to 2048 classes a row sits in the registers of a
+// group of lanes; longer rows are streamed by a workgroup, or by several
+// where rows are few, each with running statistics per lane.
+//
+// The top alternatives of a streamed row come from lists: each wave appends
+// what exceeds the least of its best `top` values so far, which after the
+// first few hundred elements is rare, and shrinks its list to the best
+// whenever it fills.  A wave meets its elements in ascending order, so that an
+// equal value met later is rightly left out: ties go to the lowest index.
+#include "oc_rows.h"
+#include "oc_sequence.h"
+
+namespace oci {
+namespace {
+
+using namespace ocr;
+
+constexpr float kLog2e = 1.4426950408889634f;
+#define OC_INF __builtin_inff()
+constexpr int kNone = 0x7fffffff;   // index of no element
+constexpr int kCap = 1024;          // entries of a wave's list
+constexpr int kStep = 512;          // elements that a wave takes at a time
+
+__device__ __forceinline__ int lane() { return (int)(threadIdx.x & 63); }
+__device__ __forceinline__ int wave() { return __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)); }
+
+// exp(z), and z bounded for the product exp(z) z, which is 0 at -infinity.
+__device__ __forceinline__ float expn(float z) { return __builtin_amdgcn_exp2f(z * kLog2e); }
+__device__ __forceinline__ float bounded(float z) { return fmaxf(z, -1e4f); }
+
+// Running maximum, sum of exponentials and of exponentials times exponents.
+struct Stat {
+  float m = -OC_INF, s = 0.f, t = 0.f;
+
+  __device__ __forceinline__ void rescale(float now) {
+    if (now == m || m == -OC_INF) {
+      m = now;
+      return;
+    }
+    const float d = m - now, f = expn(d);
+    t = f * (t + s * bounded(d));
+    s *= f;
+    m = now;
+  }
+  __device__ __forceinline__ void add(float x) {
+    const float z = x - m, e = expn(z);
+    s += e;
+    t += e * bounded(z);
+  }
+  __device__ __forceinline__ void join(Stat o) {
+    const float now = fmaxf(m, o.m);
+    rescale(now);
+    o.rescale(now);
+    s += o.s;
+    t += o.t;
+  }
+};
+
+__device__ __forceinline__ Stat group_stat(Stat a, int width) {
+  for (int i = width >> 1; i; i >>= 1) {
+    Stat o;
+    o.m = __shfl_xor(a.m, i);
+    o.s = __shfl_xor(a.s, i);
+    o.t = __shfl_xor(a.t, i);
+    a.join(o);
+  }
+  return a;
+}
+
+// Better first: greater value, then lower index.
+__device__ __forceinline__ bool better(float v, int i, float w, int j) { return v > w || (v == w && i < j); }
+
+__device__ __forceinline__ void group_best(float& v, int& i, int width) {
+  for (int k = width >> 1; k; k >>= 1) {
+    const float w = __shfl_xor(v, k);
+    const int j = __shfl_xor(i, k);
+    if (better(w, j, v, i)) {
+      v = w;
+      i = j;
+    }
+  }
+}
+
+// What a row's statistics say of its label.
+__device__ __forceinline__ void write_row(const LabelArgs& a, int64_t row, const Stat& st, float lse, float mine) {
+  a.lse[row] = lse;
+  const bool none = st.m == -OC_INF && st.s == 0.f;  // every class ruled out
+  const int label = a.labels[row];
+  a.logprob[row] = label < 0 || label >= a.classes ? 0.f : none ? -OC_INF : mine - lse;
+  if (a.entropy) {
+    const float h = logf(st.s) - st.t / st.s;
+    a.entropy[row] = none || h < 0.f ? 0.f : h;
+  }
+}
+
+__device__ __forceinline__ float lse_of(const Stat& st) { return st.m == -OC_INF && st.s == 0.f ? -OC_INF : st.m + logf(st.s); }
+
+template <class T>
+__device__ __forceinline__ float label_logit(const LabelArgs& a, int64_t row) {
+  const int label = a.labels[row];
+  return label < 0 || label >= a.classes ? 0.f : (float)((const T*)a.logits)[row * a.classes + label];
+}
+
+__device__ __forceinline__ void write_top(const LabelArgs& a, int64_t row, int k, float v, int i, float lse) {
+  a.top_label[row * a.top + k] = i == kNone ? -1 : i;
+  a.top_logprob[row * a.top + k] = i == kNone ? __builtin_nanf("") : v == -OC_INF ? v : v - lse;
+}
+
+// ---------------------------------------------------------------------------
+// Rows in registers: `lanes` lanes, NV vectors of eight
+// ---------------------------------------------------------------------------
+
+template <class T, bool VEC, int NV>
+struct Held {
+  f32x8 x[NV];
+  int t, lanes, c;
+
+  __device__ __forceinline__ int at(int v, int i) const { return VEC ? 8 * (v * lanes + t) + i : (8 * v + i) * lanes + t; }
+  // Elements past the row are -infinity.
+  __device__ __forceinline__ void load(const T* row) {
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[v][i] = -OC_INF;
+      if constexpr (VEC) {
+        if (at(v, 0) < c) x[v] = load8(row + at(v, 0));
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (at(v, i) < c) x[v][i] = (float)row[at(v, i)];
+      }
+    }
+  }
+  __device__ __forceinline__ void store(T* row) const {
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      if constexpr (VEC) {
+        if (at(v, 0) < c) store8(row + at(v, 0), x[v]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (at(v, i) < c) store1(row + at(v, i), x[v][i]);
+      }
+    }
+  }
+};
+
+template <class T, bool VEC, int NV>
+__global__ __launch_bounds__(256) void k_labels_held(LabelArgs a) {
+  const int per = 256 / a.lanes, mine = (int)threadIdx.x / a.lanes;
+  Held<T, VEC, NV> r;
+  r.t = (int)threadIdx.x & (a.lanes - 1);
+  r.lanes = a.lanes;
+  r.c = a.classes;
+  for (int64_t first = (int64_t)blockIdx.x * per; first < a.rows; first += (int64_t)gridDim.x * per) {
+    const int64_t row = first + mine;
+    if (row >= a.rows) continue;  // whole groups of lanes: the exchanges below stay within one
+    r.load((const T*)a.logits + row * a.classes);
+    Stat st;
+    float m = -OC_INF;
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) m = fmaxf(m, r.x[v][i]);
+    m = group_max(m, a.lanes);
+    st.m = m;
+    if (m != -OC_INF) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) st.add(r.x[v][i]);
+    } else {
+      // Nothing but -infinity, or NaN, which must show.
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) st.s += r.x[v][i] != r.x[v][i] ? r.x[v][i] : 0.f;
+    }
+    st.s = group_sum(st.s, a.lanes);
+    st.t = group_sum(st.t, a.lanes);
+    const float lse = lse_of(st);
+    if (r.t == 0) write_row(a, row, st, lse, label_logit<T>(a, row));
+    // The best of what comes after the last one found.
+    float last = OC_INF;
+    int last_i = -1;
+    for (int k = 0; k < a.top; ++k) {
+      float best = -OC_INF;
+      int best_i = kNone;
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int j = r.at(v, i);
+          const float x = r.x[v][i];
+          if (j < a.classes && better(last, last_i, x, j) && better(x, j, best, best_i)) {
+            best = x;
+            best_i = j;
+          }
+        }
+      group_best(best, best_i, a.lanes);
+      if (r.t == 0) write_top(a, row, k, best, best_i, lse);
+      last = best;
+      last_i = best_i;
+    }
+  }
+}
+
+// Gradient of one element; none: the row has no class left.
+struct Grad {
+  float lse, g, ge, h;
+  bool none;
+  __device__ __forceinline__ float operator()(float x) const {
+    const float z = x - lse;
+    return none ? 0.f : -expn(z) * (g + ge * (bounded(z) + h));
+  }
+};
+
+__device__ __forceinline__ Grad row_grad(const LabelArgs& a, int64_t row, int* label) {
+  Grad d;
+  d.lse = a.lse[row];
+  d.none = d.lse == -OC_INF;
+  *label = a.labels[row];
+  if (*label >= a.classes || d.none) *label = -1;
+  d.g = *label < 0 || !a.dlogprob ? 0.f : a.dlogprob[row];
+  d.ge = a.dentropy ? a.dentropy[row] : 0.f;
+  d.h = a.dentropy ? a.entropy[row] : 0.f;
+  return d;
+}
+
+template <class T, bool VEC, int NV>
+__global__ __launch_bounds__(256) void k_labels_back_held(LabelArgs a) {
+  const int per = 256 / a.lanes, mine = (int)threadIdx.x / a.lanes;
+  Held<T, VEC, NV> r;
+  r.t = (int)threadIdx.x & (a.lanes - 1);
+  r.lanes = a.lanes;
+  r.c = a.classes;
+  for (int64_t first = (int64_t)blockIdx.x * per; first < a.rows; first += (int64_t)gridDim.x * per) {
+    const int64_t row = first + mine;
+    if (row >= a.rows) continue;
+    r.load((const T*)a.logits + row * a.classes);
+    int label;
+    const Grad d = row_grad(a, row, &label);
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) r.x[v][i] = d(r.x[v][i]) + (r.at(v, i) == label ? d.g : 0.f);
+    r.store((T*)a.dlogits + row * a.classes);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Long rows, streamed
+// ---------------------------------------------------------------------------
+
+// A wave's list of candidates in LDS and what it takes to enter it.
+struct List {
+  float* v;
+  int* i;
+  int count, next;
+  float least;
+
+  // Appends this lane's x, element index j, where `take`.
+  __device__ __forceinline__ void push(bool take, float x, int j) {
+    const uint64_t all = __ballot(take);
+    if (take) {
+      const int at = count + __builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, 0));
+      v[at] = x;
+      i[at] = j;
+    }
+    count += __popcll(all);
+  }
+
+  // The list's `top` best, in order, at its front.  n <= kCap entries.
+  __device__ __forceinline__ void shrink(int top) {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    float x[kCap / 64];
+    int j[kCap / 64];
+#pragma unroll
+    for (int k = 0; k < kCap / 64; ++k) {
+      const int at = lane() + 64 * k;
+      x[k] = at < count ? v[at] : -OC_INF;
+      j[k] = at < count ? i[at] : kNone;
+    }
+    __builtin_amdgcn_wave_barrier();
+    float last = OC_INF;
+    int last_i = -1, found = 0;
+    for (int k = 0; k < top; ++k) {
+      float best = -OC_INF;
+      int best_i = kNone;
+#pragma unroll
+      for (int e = 0; e < kCap / 64; ++e)
+        if (j[e] != kNone && better(last, last_i, x[e], j[e]) && better(x[e], j[e], best, best_i)) {
+          best = x[e];
+          best_i = j[e];
+        }
+      group_best(best, best_i, 64);
+      best_i = __builtin_amdgcn_readfirstlane(best_i);
+      if (best_i == kNone) break;
+      if (lane() == 0) {
+        v[k] = best;
+        i[k] = best_i;
+      }
+      last = best;
+      last_i = best_i;
+      found = k + 1;
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    count = found;
+    least = found == top ? last : -OC_INF;
+    next = kCap - kStep;
+  }
+};
+
+// Elements of a row range before the first 16-byte boundary.
+template <class T>
+__device__ __forceinline__ int head_of(const T* p, int n) {
+  const int h = (int)(((16 - ((uintptr_t)p & 15)) & 15) / sizeof(T));
+  return h < n ? h : n;
+}
+
+// Writes the top entries; where fewer elements than that are above -infinity
+// the first of the others fill up, in order.
+template <class T>
+__device__ __forceinline__ void finish_top(const LabelArgs& a, int64_t row, const float* v, const int* i, int count,
+                                           float lse) {
+  if (lane() < count) write_top(a, row, lane(), v[lane()], i[lane()], lse);
+  const T* x = (const T*)a.logits + row * a.classes;
+  for (int64_t j = 0; count < a.top && j < a.classes; j += 64) {
+    const bool hit = j + lane() < a.classes && (float)x[j + lane()] == -OC_INF;
+    const uint64_t all = __ballot(hit);
+    const int at = count + __builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, 0));
+    if (hit && at < a.top) write_top(a, row, at, -OC_INF, (int)(j + lane()), lse);
+    count += __popcll(all);
+  }
+  if (lane() >= count && lane() < a.top) write_top(a, row, lane(), 0.f, kNone, lse);
+}
+
+// One workgroup per row (blockIdx.x) and part of it (blockIdx.y).  Writes the
+// row's results, or where a row has several parts their statistics and lists.
+template <class T, bool TOP>
+__global__ __launch_bounds__(256) void k_labels_streamed(LabelArgs a) {
+  __shared__ float vals[TOP ? 4 * kCap : 1];
+  __shared__ int idxs[TOP ? 4 * kCap : 1];
+  __shared__ float stats[3][4];
+  const int64_t row = blockIdx.x;
+  const int j0 = (int)blockIdx.y * a.per, j1 = j0 + a.per < a.classes ? j0 + a.per : a.classes;
+  const T* x = (const T*)a.logits + row * a.classes + j0;
+  const int n = j1 - j0, head = head_of(x, n), body = (n - head) / 8, w = wave();
+  List list{vals + (TOP ? w * kCap : 0), idxs + (TOP ? w * kCap : 0), 0, 1, -OC_INF};
+  Stat st;
+
+  const auto one = [&](bool in, int j) {
+    const float y = in ? (float)x[j] : -OC_INF;
+    if (y > st.m) st.rescale(y);
+    if (in && (st.m != -OC_INF || y != y)) st.add(y);
+    if (TOP) list.push(in && y > list.least, y, j0 + j);
+  };
+  if (w == 0 && head) one(lane() < head, lane());
+  for (int v = (int)threadIdx.x; v - lane() < body; v += 256) {
+    f32x8 y;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = -OC_INF;
+    if (v < body) y = load8(x + head + 8 * (int64_t)v);
+    float top = y[0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) top = fmaxf(top, y[i]);
+    if (top > st.m) st.rescale(top);
+    // A maximum of -infinity so far: only NaN counts.
+    const float base = st.m == -OC_INF ? 0.f : st.m;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float z = y[i] - base, e = expn(z);
+      st.s += e;
+      st.t += e * bounded(z);
+    }
+    if constexpr (TOP) {
+      if (__ballot(top > list.least)) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) list.push(y[i] > list.least, y[i], j0 + head + 8 * v + i);
+        if (list.count >= list.next) list.shrink(a.top);
+      }
+    }
+  }
+  // The last wave takes the elements past the last whole vector.
+  const int tail = head + 8 * body;
+  if (w == 3 && tail < n) one(tail + lane() < n, tail + lane());
+
+  st = group_stat(st, 64);
+  if (lane() == 0) {
+    stats[0][w] = st.m;
+    stats[1][w] = st.s;
+    stats[2][w] = st.t;
+  }
+  if (TOP) list.shrink(a.top);
+  __shared__ int counts[4];
+  if (TOP && lane() == 0) counts[w] = list.count;
+  __syncthreads();
+  if (w) return;
+  for (int i = 1; i < 4; ++i) {
+    Stat o;
+    o.m = stats[0][i];
+    o.s = stats[1][i];
+    o.t = stats[2][i];
+    st.join(o);
+  }
+  if constexpr (TOP) {
+    for (int k = 1; k < 4; ++k) {
+      const bool in = lane() < counts[k];
+      list.push(in, in ? vals[k * kCap + lane()] : 0.f, in ? idxs[k * kCap + lane()] : 0);
+    }
+    list.shrink(a.top);
+  }
+  if (a.parts > 1) {
+    const int64_t p = row * a.parts + blockIdx.y;
+    if (lane() == 0) {
+      a.part_stat[3 * p] = st.m;
+      a.part_stat[3 * p + 1] = st.s;
+      a.part_stat[3 * p + 2] = st.t;
+    }
+    if (TOP && lane() < a.top) {
+      const bool in = lane() < list.count;
+      a.part_val[p * a.top + lane()] = in ? list.v[lane()] : -OC_INF;
+      a.part_idx[p * a.top + lane()] = in ? list.i[lane()] : kNone;
+    }
+    return;
+  }
+  const float lse = lse_of(st);
+  if (lane() == 0) write_row(a, row, st, lse, label_logit<T>(a, row));
+  if constexpr (TOP) finish_top<T>(a, row, list.v, list.i, list.count, lse);
+}
+
+// Joins the parts of a row: one wave per row.
+template <class T, bool TOP>
+__global__ __launch_bounds__(64) void k_labels_join(LabelArgs a) {
+  __shared__ float vals[TOP ? kCap : 1];
+  __shared__ int idxs[TOP ? kCap : 1];
+  const int64_t row = blockIdx.x;
+  Stat st;
+  for (int p = lane(); p < a.parts; p += 64) {
+    Stat o;
+    const float* q = a.part_stat + 3 * (row * a.parts + p);
+    o.m = q[0];
+    o.s = q[1];
+    o.t = q[2];
+    st.join(o);
+  }
+  st = group_stat(st, 64);
+  const float lse = lse_of(st);
+  if (lane() == 0) write_row(a, row, st, lse, label_logit<T>(a, row));
+  if constexpr (TOP) {
+    List list{vals, idxs, 0, 1, -OC_INF};
+    const int n = a.parts * a.top;
+    for (int e = 0; e < n; e += 64) {
+      if (list.count > kCap - 64) list.shrink(a.top);
+      const bool in = e + lane() < n;
+      const int64_t at = row * n + e + lane();
+      const float v = in ? a.part_val[at] : 0.f;
+      const int i = in ? a.part_idx[at] : kNone;
+      list.push(i != kNone, v, i);
+    }
+    list.shrink(a.top);
+    finish_top<T>(a, row, list.v, list.i, list.count, lse);
+  }
+}
+
+// Rows (blockIdx.x, with a stride) and ranges of a.per elements of them
+// (blockIdx.y).  `same`: logits and dlogits lie alike to 16 bytes.
+template <class T>
+__global__ __launch_bounds__(256) void k_labels_back_streamed(LabelArgs a, bool same) {
+  const int64_t row = blockIdx.x;
+  const int j0 = (int)blockIdx.y * a.per, j1 = j0 + a.per < a.classes ? j0 + a.per : a.classes;
+  const T* x = (const T*)a.logits + row * a.classes + j0;
+  T* y = (T*)a.dlogits + row * a.classes + j0;
+  int label;
+  const Grad d = row_grad(a, row, &label);
+  label -= j0;
+  const int n = j1 - j0, head = same ? head_of(x, n) : 0, body = same ? (n - head) / 8 : 0, tail = head + 8 * body;
+  const auto one = [&](int j) { store1(y + j, d((float)x[j]) + (j == label ? d.g : 0.f)); };
+  if ((int)threadIdx.x < head) one((int)threadIdx.x);
+  for (int v = (int)threadIdx.x; v < body; v += 256) {
+    f32x8 g = load8(x + head + 8 * (int64_t)v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) g[i] = d(g[i]) + (head + 8 * v + i == label ? d.g : 0.f);
+    store8(y + head + 8 * (int64_t)v, g);
+  }
+  for (int j = tail + (int)threadIdx.x; j < n; j += 256) one(j);
+}
+
+// ---------------------------------------------------------------------------
+// Launches
+// ---------------------------------------------------------------------------
+
+constexpr int kHeld = 2048;  // classes that a group of lanes holds
+
+int lanes_of(int classes) {
+  const int n = (classes + (classes <= 512 ? 7 : 31)) / (classes <= 512 ? 8 : 32);
+  int lanes = 1;
+  while (lanes < n) lanes <<= 1;
+  return lanes;
+}
+
+template <class F>
+hipError_t by_held(int classes, bool vec, F f) {
+  using One = std::integral_constant<int, 1>;
+  using Four = std::integral_constant<int, 4>;
+  if (vec) return classes <= 512 ? f(std::true_type(), One()) : f(std::true_type(), Four());
+  return classes <= 512 ? f(std::false_type(), One()) : f(std::false_type(), Four());
+}
+
+unsigned held_grid(int64_t rows, int lanes) {
+  const int64_t n = (rows + 256 / lanes - 1) / (256 / lanes);
+  return (unsigned)(n < 256 * 16 ? n : 256 * 16);
+}
+
+}  // namespace
+
+// Parts of a streamed row: enough workgroups to fill the device, each with
+// at least two steps of its four waves.
+int label_parts(int64_t rows, int classes) {
+  if (rows <= 0 || classes <= kHeld) return 1;
+  const int64_t most = classes / (8 * kStep);
+  int64_t n = 1024 / rows;
+  if (n > most) n = most;
+  if (n > 64) n = 64;
+  return n < 1 ? 1 : (int)n;
+}
+
+hipError_t launch_labels(LabelArgs a, int dtype, hipStream_t s) {
+  return by_type(dtype, [&](auto t) {
+    using T = decltype(t);
+    if (a.classes <= kHeld) {
+      a.lanes = lanes_of(a.classes);
+      return by_held(a.classes, a.classes % 8 == 0 && ok16(a.logits), [&](auto v, auto nv) {
+        k_labels_held<T, decltype(v)::value, decltype(nv)::value><<<held_grid(a.rows, a.lanes), 256, 0, s>>>(a);
+        return hipGetLastError();
+      });
+    }
+    a.parts = label_parts(a.rows, a.classes);
+    a.per = (a.classes + a.parts - 1) / a.parts;
+    const dim3 grid((unsigned)a.rows, (unsigned)a.parts);
+    if (a.top)
+      k_labels_streamed<T, true><<<grid, 256, 0, s>>>(a);
+    else
+      k_labels_streamed<T, false><<<grid, 256, 0, s>>>(a);
+    const hipError_t err = hipGetLastError();
+    if (err != hipSuccess || a.parts == 1) return err;
+    if (a.top)
+      k_labels_join<T, true><<<(unsigned)a.rows, 64, 0, s>>>(a);
+    else
+      k_labels_join<T, false><<<(unsigned)a.rows, 64, 0, s>>>(a);
+    return hipGetLastError();
+  });
+}
+
+hipError_t launch_labels_back(LabelArgs a, int dtype, hipStream_t s) {
+  return by_type(dtype, [&](auto t) {
+    using T = decltype(t);
+    if (a.classes <= kHeld) {
+      a.lanes = lanes_of(a.classes);
+      return by_held(a.classes, a.classes % 8 == 0 && ok16(a.logits) && ok16(a.dlogits), [&](auto v, auto nv) {
+        k_labels_back_held<T, decltype(v)::value, decltype(nv)::value><<<held_grid(a.rows, a.lanes), 256, 0, s>>>(a);
+        return hipGetLastError();
+      });
+    }
+    a.per = 16384;
+    const dim3 grid((unsigned)a.rows, (unsigned)((a.classes + a.per - 1) / a.per));
+    k_labels_back_streamed<T><<<grid, 256, 0, s>>>(a, (((uintptr_t)a.logits ^ (uintptr_t)a.dlogits) & 15) == 0);
+    return hipGetLastError();
+  });
+}
+
+}  // namespace oci

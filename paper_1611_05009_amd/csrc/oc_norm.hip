@@ -1,0 +1,306 @@
+// Root-mean-square norm of rows, with the residual's addition before it and an
+// optional output in 8 bits, and its gradients.
+//
+//   h = x + residual,  r = 1 / sqrt(mean(h^2) + eps),  y = h r w;
+//   dx = dsum + r (w dy) - h r^3 mean(w dy h),  dw = sum over rows of dy h r.
+//
+// Memory bound: every input is read once and held in registers (32 values per
+// lane at most) between the row's reduction and its outputs.  A row belongs to
+// `lanes` lanes of a wave (narrow rows share a wave), or to a whole
+// workgroup of up to 1024 threads.  Workgroups walk the rows with a stride
+// and keep their columns' weights in registers.
+#include "oc_internal.h"
+#include "oc_rows.h"
+#include "oc_sequence.h"
+
+namespace oci {
+namespace {
+
+using namespace ocr;
+
+// A row's elements in one lane: NV vectors of eight.  VEC: vector v of lane t
+// holds elements 8 (v lanes + t) onwards, in one access.  Otherwise (widths
+// that are no multiple of eight, unaligned bases) eight accesses, element i of
+// vector v being (8 v + i) lanes + t: neighbouring lanes read neighbours.
+template <bool VEC>
+struct Cols {
+  int t, lanes, c;
+  __device__ __forceinline__ int at(int v, int i) const { return VEC ? 8 * (v * lanes + t) + i : (8 * v + i) * lanes + t; }
+
+  template <class T>
+  __device__ __forceinline__ f32x8 load(const T* row, int v) const {
+    f32x8 x = {0, 0, 0, 0, 0, 0, 0, 0};
+    if constexpr (VEC) {
+      if (at(v, 0) < c) x = load8(row + at(v, 0));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (at(v, i) < c) x[i] = (float)row[at(v, i)];
+    }
+    return x;
+  }
+  template <class T>
+  __device__ __forceinline__ void store(T* row, int v, f32x8 x) const {
+    if constexpr (VEC) {
+      if (at(v, 0) < c) store8(row + at(v, 0), x);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (at(v, i) < c) store1(row + at(v, i), x[i]);
+    }
+  }
+};
+
+// Reduction over a row's lanes; WIDE: over the workgroup, through LDS (two
+// barriers, so that the next reduction may reuse `part`).
+template <bool WIDE, bool MAX>
+__device__ __forceinline__ float row_reduce(float x, int lanes, float* part) {
+  x = MAX ? group_max(x, WIDE ? 64 : lanes) : group_sum(x, WIDE ? 64 : lanes);
+  if constexpr (WIDE) {
+    const int w = (int)threadIdx.x >> 6, n = (int)blockDim.x >> 6;
+    if ((threadIdx.x & 63) == 0) part[w] = x;
+    __syncthreads();
+    x = part[0];
+    for (int i = 1; i < n; ++i) x = MAX ? fmaxf(x, part[i]) : x + part[i];
+    __syncthreads();
+  }
+  return x;
+}
+
+template <class TX, class TS, class TY, bool VEC, int NV, bool WIDE>
+__global__ __launch_bounds__(WIDE ? 1024 : 256) void k_rms_norm(NormArgs a) {
+  __shared__ float part[16];
+  const int lanes = WIDE ? (int)blockDim.x : a.lanes;
+  const int per = WIDE ? 1 : 256 / lanes;  // rows of the workgroup
+  const Cols<VEC> col{WIDE ? (int)threadIdx.x : (int)threadIdx.x & (lanes - 1), lanes, a.c};
+  const int mine = WIDE ? 0 : (int)threadIdx.x / lanes;
+  f32x8 w[NV];
+#pragma unroll
+  for (int v = 0; v < NV; ++v) w[v] = col.load(a.weight, v);
+  const float inv_c = 1.f / (float)a.c;
+  for (int64_t first = (int64_t)blockIdx.x * per; first < a.rows; first += (int64_t)gridDim.x * per) {
+    const int64_t row = first + mine;
+    const bool live = row < a.rows;
+    const int64_t at = (live ? row : a.rows - 1) * a.c;
+    f32x8 x[NV];
+    float sq = 0.f;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) x[v] = col.load((const TX*)a.x + at, v);
+    if (a.residual) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v) x[v] += col.load((const TS*)a.residual + at, v);
+    }
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sq += x[v][i] * x[v][i];
+    if (a.sum && live) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v) col.store((TS*)a.sum + at, v, x[v]);
+    }
+    sq = row_reduce<WIDE, false>(sq, lanes, part);
+    const float r = 1.f / sqrtf(sq * inv_c + a.eps);
+    float most = 0.f;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      x[v] = x[v] * r * w[v];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(x[v][i]));
+    }
+    if constexpr (sizeof(TY) == 1) {
+      // The row's largest value stands at 448, the largest of the 8-bit type.
+      most = row_reduce<WIDE, true>(most, lanes, part);
+      const float scale = most > 0.f ? most / 448.f : 1.f, inv = 1.f / scale;
+#pragma unroll
+      for (int v = 0; v < NV; ++v) x[v] *= inv;
+      if (live && col.t == 0) a.scale[row] = scale;
+    }
+    if (live) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v) col.store((TY*)a.y + at, v, x[v]);
+    }
+  }
+}
+
+// Workgroup g adds up dy h r over its rows; k_norm_dweight adds the groups'
+// sums [groups][c] in order.
+template <class TS, class TY, bool VEC, int NV, bool WIDE>
+__global__ __launch_bounds__(WIDE ? 1024 : 256) void k_rms_norm_back(NormArgs a) {
+  __shared__ float part[16];
+  __shared__ float add[WIDE ? 1 : 256 * 8];
+  const int lanes = WIDE ? (int)blockDim.x : a.lanes;
+  const int per = WIDE ? 1 : 256 / lanes;
+  const Cols<VEC> col{WIDE ? (int)threadIdx.x : (int)threadIdx.x & (lanes - 1), lanes, a.c};
+  const int mine = WIDE ? 0 : (int)threadIdx.x / lanes;
+  f32x8 w[NV], dw[NV];
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    w[v] = col.load(a.weight, v);
+    dw[v] = f32x8{0, 0, 0, 0, 0, 0, 0, 0};
+  }
+  const float inv_c = 1.f / (float)a.c;
+  for (int64_t first = (int64_t)blockIdx.x * per; first < a.rows; first += (int64_t)gridDim.x * per) {
+    const int64_t row = first + mine;
+    const bool live = row < a.rows;
+    const int64_t at = (live ? row : a.rows - 1) * a.c;
+    f32x8 h[NV], d[NV];
+    float sq = 0.f, dot = 0.f;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      h[v] = col.load((const TS*)a.sum + at, v);
+      d[v] = col.load((const TY*)a.dy + at, v);
+    }
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        sq += h[v][i] * h[v][i];
+        dot += d[v][i] * w[v][i] * h[v][i];
+      }
+    sq = row_reduce<WIDE, false>(sq, lanes, part);
+    dot = row_reduce<WIDE, false>(dot, lanes, part);
+    const float r = 1.f / sqrtf(sq * inv_c + a.eps);
+    const float k = dot * inv_c * r * r;  // mean(u n) of u = w dy, n = h r, over r
+    if (live) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        dw[v] += d[v] * (h[v] * r);
+        f32x8 g = (d[v] * w[v] - h[v] * k) * r;
+        if (a.dsum) g += col.load((const TS*)a.dsum + at, v);
+        col.store((TS*)a.dx + at, v, g);
+      }
+    }
+  }
+  if (!a.part) return;
+  float* out = a.part + (int64_t)blockIdx.x * a.c;
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    f32x8 s = dw[v];
+    if constexpr (!WIDE) {
+      // The workgroup's rows in order.
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < 8; ++i) add[i * 256 + threadIdx.x] = s[i];
+      __syncthreads();
+      if (mine == 0) {
+        for (int j = 1; j < per; ++j)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) s[i] += add[i * 256 + threadIdx.x + j * lanes];
+      }
+    }
+    if (mine == 0) col.store(out, v, s);
+  }
+}
+
+// Columns' sums over the groups: 16 columns of a workgroup, 64 threads each.
+__global__ __launch_bounds__(1024) void k_norm_dweight(const float* part, int groups, int c, float* dw) {
+  __shared__ float add[64][17];
+  const int x = (int)threadIdx.x & 15, y = (int)threadIdx.x >> 4, at = (int)blockIdx.x * 16 + x;
+  float s = 0.f;
+  if (at < c)
+    for (int g = y; g < groups; g += 64) s += part[(int64_t)g * c + at];
+  add[y][x] = s;
+  __syncthreads();
+  for (int n = 32; n; n >>= 1) {
+    if (y < n) add[y][x] += add[y + n][x];
+    __syncthreads();
+  }
+  if (y == 0 && at < c) dw[at] = add[0][x];
+}
+
+// Lanes per row, vectors per lane and workgroup size by width.
+struct Shape {
+  int nv, lanes, threads;
+  bool wide;
+};
+
+Shape shape_of(int c) {
+  Shape s{1, 1, 256, false};
+  s.nv = c <= 512 ? 1 : 4;
+  const int n = (c + 8 * s.nv - 1) / (8 * s.nv);
+  while (s.lanes < n) s.lanes <<= 1;
+  if (s.lanes > 64) {
+    s.wide = true;
+    s.threads = s.lanes;
+  }
+  return s;
+}
+
+template <class F>
+hipError_t by_shape(const Shape& s, bool vec, F f) {
+  const auto go = [&](auto v) {
+    if (s.wide) return f(v, std::integral_constant<int, 4>(), std::true_type());
+    if (s.nv == 4) return f(v, std::integral_constant<int, 4>(), std::false_type());
+    return f(v, std::integral_constant<int, 1>(), std::false_type());
+  };
+  return vec ? go(std::true_type()) : go(std::false_type());
+}
+
+int64_t row_groups(const Shape& s, int64_t rows) { return s.wide ? rows : (rows + 256 / s.lanes - 1) / (256 / s.lanes); }
+
+}  // namespace
+
+// Workgroups of the gradient: enough to fill the device, few enough for the
+// partial sums of dweight to stay small beside the rows.
+int norm_back_groups(int64_t rows, int c) {
+  const Shape s = shape_of(c);
+  const int64_t n = row_groups(s, rows), most = s.wide ? 256 * (1024 / s.threads < 8 ? 1024 / s.threads : 8) : 1024;
+  return (int)(n < most ? n : most);
+}
+
+hipError_t launch_rms_norm(NormArgs a, int x_type, int sum_type, int y_type, hipStream_t s) {
+  const Shape sh = shape_of(a.c);
+  a.lanes = sh.lanes;
+  const bool vec = a.c % 8 == 0 && ok16(a.x) && ok16(a.residual) && ok16(a.weight) && ok16(a.sum) && ok16(a.y);
+  const int64_t n = row_groups(sh, a.rows);
+  const unsigned grid = (unsigned)(n < 256 * 16 ? n : 256 * 16);
+  return by_type(x_type, [&](auto tx) {
+    using TX = decltype(tx);
+    const auto sums = [&](auto ts) {
+      using TS = decltype(ts);
+      return by_shape(sh, vec, [&](auto v, auto nv, auto wide) {
+        constexpr bool V = decltype(v)::value, W = decltype(wide)::value;
+        constexpr int N = decltype(nv)::value;
+        const auto go = [&](auto ty) {
+          k_rms_norm<TX, TS, decltype(ty), V, N, W><<<grid, sh.threads, 0, s>>>(a);
+          return hipGetLastError();
+        };
+        if (y_type == kF8) return go(e4m3());
+        if constexpr (sizeof(TX) == 4) {
+          if (y_type == kF16) return go(_Float16());
+          if (y_type == kBF16) return go(__bf16());
+        }
+        return go(TX());
+      });
+    };
+    if constexpr (sizeof(TX) == 2) {
+      if (sum_type != kF32) return sums(TX());
+    }
+    return sums(float());
+  });
+}
+
+hipError_t launch_rms_norm_back(NormArgs a, int sum_type, int y_type, float* dweight, hipStream_t s) {
+  const Shape sh = shape_of(a.c);
+  a.lanes = sh.lanes;
+  const bool vec = a.c % 8 == 0 && ok16(a.sum) && ok16(a.dy) && ok16(a.weight) && ok16(a.dsum) && ok16(a.dx) && ok16(a.part);
+  const int groups = norm_back_groups(a.rows, a.c);
+  const auto run = [&](auto ts, auto ty) {
+    return by_shape(sh, vec, [&](auto v, auto nv, auto wide) {
+      k_rms_norm_back<decltype(ts), decltype(ty), decltype(v)::value, decltype(nv)::value, decltype(wide)::value>
+          <<<(unsigned)groups, sh.threads, 0, s>>>(a);
+      return hipGetLastError();
+    });
+  };
+  const hipError_t err = a.rows == 0 ? hipSuccess : by_type(y_type, [&](auto ty) {
+    if constexpr (sizeof(ty) == 2) {
+      if (sum_type != kF32) return run(ty, ty);
+    }
+    return run(float(), ty);
+  });
+  if (err != hipSuccess || !dweight) return err;
+  k_norm_dweight<<<(unsigned)((a.c + 15) / 16), 1024, 0, s>>>(a.part, groups, a.c, dweight);
+  return hipGetLastError();
+}
+
+}  // namespace oci

@@ -21,7 +21,7 @@ LIB_PATH = os.path.join(_HERE, "liboctnet_hip.so")
 OC_OK = 0
 OC_SPLIT_MIXED, OC_SPLIT_ANY = 0, 1
 OC_POOL_AVG, OC_POOL_MAX = 0, 1
-OC_F32, OC_F16, OC_BF16 = 0, 1, 2
+OC_F32, OC_F16, OC_BF16, OC_F8 = 0, 1, 2, 3
 OC_CONV_AUTO, OC_CONV_GENERIC, OC_CONV_MFMA, OC_CONV_GEMM, OC_CONV_TRUNCATED = 0, 1, 2, 3, 4
 
 _IMPL = {"auto": OC_CONV_AUTO, "generic": OC_CONV_GENERIC, "mfma": OC_CONV_MFMA, "gemm": OC_CONV_GEMM,
@@ -83,6 +83,14 @@ SIGNATURES = {
     "oc_attention_backward_workspace": (_I, [_L, _L, _I, _I, _I, _I, _P]),
     "oc_attention_backward": (_I, [_P, _L, _L, _P, _L, _L, _P, _L, _L, _P, _P, _P, _P, _P, _I, _L, _L, _I, _I, _I,
                                    _I, _F, _I, _P, _P, _P, _P, _S, _P]),
+    "oc_rms_norm": (_I, [_P, _I, _P, _I, _P, _L, _I, _F, _P, _P, _I, _P, _P]),
+    "oc_rms_norm_backward_workspace": (_I, [_L, _I, _P]),
+    "oc_rms_norm_backward": (_I, [_P, _I, _P, _P, _I, _P, _L, _I, _F, _P, _P, _P, _S, _P]),
+    "oc_label_logprobs_workspace": (_I, [_L, _I, _I, _P]),
+    "oc_label_logprobs": (_I, [_P, _I, _P, _L, _I, _I, _P, _P, _P, _P, _P, _P, _S, _P]),
+    "oc_label_logprobs_backward": (_I, [_P, _I, _P, _L, _I, _P, _P, _P, _P, _P, _P]),
+    "oc_clip_grad_norm_workspace": (_I, [_P, _I, _P]),
+    "oc_clip_grad_norm": (_I, [_P, _P, _P, _P, _I, _F, _P, _P, _S, _P]),
 }
 
 _lib = None
@@ -616,3 +624,160 @@ def attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: t
                                        _type(q), dim ** -0.5 if scale is None else scale, int(bool(causal)), _ptr(dq),
                                        _ptr(dk), _ptr(dv), _ptr(ws), ws.numel(), _stream()), "oc_attention_backward")
     return dq, dk, dv
+
+
+def _rows(t: torch.Tensor, what: str, shape=None):
+    if t.dim() != 2 or (shape is not None and t.shape != shape):
+        raise OctNetError("%s must be [rows, width]" % what)
+
+
+def _norm_weight(weight: torch.Tensor, c: int):
+    if weight.dtype != torch.float32 or tuple(weight.shape) != (c,):
+        raise OctNetError("weight must be float32 [width]")
+    return _ptr(weight)
+
+
+def _rms_norm(x, weight, residual, eps, y, scale):
+    _rows(x, "x")
+    rows, c = x.shape
+    h = x
+    if residual is not None:
+        _rows(residual, "residual", x.shape)
+        if residual.dtype not in (x.dtype, torch.float32):
+            raise OctNetError("the residual must be of x's type or float32")
+        h = torch.empty_like(residual)
+    _check(lib().oc_rms_norm(_ptr(x), _type(x), _ptr(residual), _type(h), _norm_weight(weight, c), rows, c, eps,
+                             None if residual is None else _ptr(h), _ptr(y),
+                             OC_F8 if scale is not None else _type(y), _ptr(scale), _stream()), "oc_rms_norm")
+    return h
+
+
+def rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: torch.Tensor | None = None, eps: float = 1e-6,
+             out_dtype: torch.dtype | None = None):
+    """(y, h): h = x + residual of the residual's type (x's, or float32), or x
+    itself without one; y = h / sqrt(mean(h^2) + eps) * weight per row, of
+    out_dtype (x's by default; any where x is float32).  x, residual [rows,
+    width], weight float32 [width]."""
+    y = torch.empty(x.shape, dtype=x.dtype if out_dtype is None else out_dtype, device=x.device)
+    return y, _rms_norm(x, weight, residual, eps, y, None)
+
+
+def rms_norm_8bit(x: torch.Tensor, weight: torch.Tensor, residual: torch.Tensor | None = None, eps: float = 1e-6):
+    """(y, scale, h) as rms_norm, y in 8 bits (float8_e4m3fn) with a scale per
+    row: y * scale[:, None] is the norm's output."""
+    y = torch.empty(x.shape, dtype=torch.float8_e4m3fn, device=x.device)
+    scale = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
+    return y, scale, _rms_norm(x, weight, residual, eps, y, scale)
+
+
+def rms_norm_backward(h: torch.Tensor, weight: torch.Tensor, dy: torch.Tensor, dsum: torch.Tensor | None = None,
+                      eps: float = 1e-6, need_weight: bool = True, ws: torch.Tensor | None = None):
+    """(dx, dweight) of rms_norm: dx [rows, width] of h's type, the gradient of
+    x and of the residual, from dy (of y's type) and dsum, the gradient that
+    reaches h by other ways (None: zero)."""
+    _rows(h, "h")
+    _rows(dy, "dy", h.shape)
+    rows, c = h.shape
+    if dsum is not None and (dsum.shape != h.shape or dsum.dtype != h.dtype):
+        raise OctNetError("dsum must be of h's shape and type")
+    dx = torch.empty_like(h)
+    dw = torch.empty(c, dtype=torch.float32, device=h.device) if need_weight else None
+    if ws is None and need_weight:
+        nb = ctypes.c_size_t(0)
+        _check(lib().oc_rms_norm_backward_workspace(rows, c, ctypes.byref(nb)), "oc_rms_norm_backward_workspace")
+        ws = torch.empty(nb.value, dtype=torch.uint8, device=h.device)
+    _check(lib().oc_rms_norm_backward(_ptr(h), _type(h), _norm_weight(weight, c), _ptr(dy), _type(dy), _ptr(dsum), rows, c,
+                                      eps, _ptr(dx), _ptr(dw), _ptr(ws), 0 if ws is None else ws.numel(), _stream()),
+           "oc_rms_norm_backward")
+    return dx, dw
+
+
+@dataclass
+class LabelLogprobs:
+    """What label_logprobs returns, per row."""
+
+    logprob: torch.Tensor                    # float32 [rows], 0 where unlabelled
+    lse: torch.Tensor                        # float32 [rows]
+    entropy: torch.Tensor | None             # float32 [rows]
+    top_logprob: torch.Tensor | None = None  # float32 [rows, top]
+    top_label: torch.Tensor | None = None    # int32 [rows, top]
+
+
+def _label_shapes(logits, labels):
+    _rows(logits, "logits")
+    if labels.dtype != torch.int32 or tuple(labels.shape) != (logits.shape[0],):
+        raise OctNetError("labels must be int32 [rows]")
+    return logits.shape
+
+
+def _row_values(t: torch.Tensor | None, rows: int, what: str):
+    if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != (rows,)):
+        raise OctNetError("%s must be float32 [rows]" % what)
+    return _ptr(t)
+
+
+def label_logprobs(logits: torch.Tensor, labels: torch.Tensor, top: int = 0, entropy: bool = True,
+                   ws: torch.Tensor | None = None) -> LabelLogprobs:
+    """Log probabilities of the labels (int32 [rows], negative: none, as
+    points_vote gives them) under logits [rows, classes], the rows' entropy and
+    their `top` (at most 32) likeliest labels, ties in index order.  A logit of
+    -infinity rules a class out."""
+    rows, classes = _label_shapes(logits, labels)
+    dev = logits.device
+    r = LabelLogprobs(torch.empty(rows, dtype=torch.float32, device=dev), torch.empty(rows, dtype=torch.float32, device=dev),
+                      torch.empty(rows, dtype=torch.float32, device=dev) if entropy else None)
+    if top:
+        r.top_logprob = torch.empty((rows, top), dtype=torch.float32, device=dev)
+        r.top_label = torch.empty((rows, top), dtype=torch.int32, device=dev)
+    nb = ctypes.c_size_t(0)
+    _check(lib().oc_label_logprobs_workspace(rows, classes, top, ctypes.byref(nb)), "oc_label_logprobs_workspace")
+    if ws is None and nb.value:
+        ws = torch.empty(nb.value, dtype=torch.uint8, device=dev)
+    _check(lib().oc_label_logprobs(_ptr(logits), _type(logits), _ptr(labels), rows, classes, top, _ptr(r.logprob),
+                                   _ptr(r.lse), _ptr(r.entropy), _ptr(r.top_logprob), _ptr(r.top_label), _ptr(ws),
+                                   0 if ws is None else ws.numel(), _stream()), "oc_label_logprobs")
+    return r
+
+
+def label_logprobs_backward(logits: torch.Tensor, labels: torch.Tensor, lse: torch.Tensor,
+                            dlogprob: torch.Tensor | None, entropy: torch.Tensor | None = None,
+                            dentropy: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
+    """Gradient with respect to the logits from those of logprob and entropy
+    (float32 [rows], None: zero); out may be the logits themselves."""
+    rows, classes = _label_shapes(logits, labels)
+    if out is None:
+        out = torch.empty_like(logits)
+    elif out.shape != logits.shape or out.dtype != logits.dtype:
+        raise OctNetError("out must be of the logits' shape and type")
+    if dentropy is not None and entropy is None:
+        raise OctNetError("dentropy needs the entropy")
+    _check(lib().oc_label_logprobs_backward(_ptr(logits), _type(logits), _ptr(labels), rows, classes,
+                                            _row_values(lse, rows, "lse"), _row_values(dlogprob, rows, "dlogprob"),
+                                            _row_values(entropy, rows, "entropy"),
+                                            _row_values(dentropy, rows, "dentropy"), _ptr(out), _stream()),
+           "oc_label_logprobs_backward")
+    return out
+
+
+def clip_grad_norm(grads, max_norm: float, out=None, ws: torch.Tensor | None = None) -> torch.Tensor:
+    """Scales the gradients (a sequence of GPU tensors, of any of the three
+    types) by min(1, max_norm / (norm + 1e-6)), in place or into `out`, and
+    returns their common norm, a float32 scalar on the GPU (nothing waits for
+    it)."""
+    grads = list(grads)
+    out = grads if out is None else list(out)
+    if len(out) != len(grads) or any(a.shape != b.shape or a.dtype != b.dtype for a, b in zip(grads, out)):
+        raise OctNetError("out must match the gradients")
+    n = len(grads)
+    norm = torch.empty((), dtype=torch.float32, device=grads[0].device if n else _dev())
+    src = (_P * n)(*[_ptr(t) for t in grads])
+    dst = src if out is grads else (_P * n)(*[_ptr(t) for t in out])
+    counts = (_L * n)(*[t.numel() for t in grads])
+    types = (_I * n)(*[_type(t) for t in grads])
+    if ws is None:
+        nb = ctypes.c_size_t(0)
+        _check(lib().oc_clip_grad_norm_workspace(counts, n, ctypes.byref(nb)), "oc_clip_grad_norm_workspace")
+        ws = torch.empty(nb.value, dtype=torch.uint8, device=norm.device)
+    _check(lib().oc_clip_grad_norm(src, dst, counts, types, n, max_norm, _ptr(norm), _ptr(ws), ws.numel(), _stream()),
+           "oc_clip_grad_norm")
+    return norm

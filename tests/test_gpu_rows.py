@@ -1,0 +1,377 @@
+"""Norms, label log probabilities and gradient clipping against their
+definitions in 64 bits.
+
+Bars.  u is the unit roundoff of the output type, U32 that of float.  A norm's
+row carries relative (c / 64 + 8) U32 at most from its sum of squares (lanes
+add c / 64 terms at least pairwise afterwards; taken as c U32 + 16 U32) and two
+roundings per factor.  Log probabilities: exponentials of relative 4 U32 plus
+|z| U32 from their argument, sums of `classes` terms, one subtraction of
+numbers of the logits' size."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from common import U32, log
+
+pytestmark = pytest.mark.gpu
+
+UNIT = {torch.float32: 2.0 ** -24, torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}
+TINY = {torch.float32: 2.0 ** -126, torch.float16: 2.0 ** -25, torch.bfloat16: 2.0 ** -126}
+TYPES = [torch.float32, torch.float16, torch.bfloat16]
+EPS = 1e-6
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+
+
+def near(got, want, bar, what):
+    got = got.cpu().double()
+    want = want.double()
+    fin = torch.isfinite(want)
+    assert torch.equal(torch.isfinite(got), fin), what + ": finite places"
+    other = ~fin & ~torch.isnan(want)
+    assert torch.equal(got[other], want[other]) and torch.equal(torch.isnan(got), torch.isnan(want)), what
+    err, bar = (got - want)[fin].abs(), bar.expand_as(want)[fin]
+    if not err.numel():
+        return
+    r = float((err / bar.clamp(min=1e-300)).masked_fill(err == 0, 0.0).max())
+    log("  %s: %.3g of the bar, largest error %.3g" % (what, r, float(err.max())))
+    assert r <= 1.0, what
+
+
+def randn(seed, *shape):
+    return torch.randn(shape, generator=torch.Generator().manual_seed(seed))
+
+
+# ---------------------------------------------------------------------------
+# Norm
+# ---------------------------------------------------------------------------
+
+WIDTHS = [1, 3, 8, 17, 64, 100, 256, 513, 520, 1000, 2048, 2056, 4099, 8192, 32768]
+
+
+def norm_inputs(rows, c, dt, st):
+    x, r = randn(c, rows, c).to(dt), (2 * randn(c + 1, rows, c)).to(st)
+    if rows > 3:
+        x[2], r[2] = 0, 0       # a row of zeros
+    return x, r, 1 + 0.3 * randn(c + 2, c)
+
+
+def norm_reference(h, w):
+    rms = (h.square().mean(1, keepdim=True) + EPS).sqrt()
+    return h / rms * w, rms
+
+
+@pytest.mark.parametrize("dt,st,ot", [(torch.float32,) * 3, (torch.bfloat16,) * 3, (torch.float16, torch.float32, torch.float16),
+                                      (torch.float32, torch.float32, torch.bfloat16), (torch.bfloat16, torch.float32, torch.bfloat16)])
+@pytest.mark.parametrize("c", WIDTHS)
+def test_norm(c, dt, st, ot):
+    from paper_1611_05009_amd import octnet as oc
+    rows = 1 if c == 32768 else 67
+    x, r, w = norm_inputs(rows, c, dt, st)
+    # in place of the last rows of a larger array: rows of odd widths lie
+    # anywhere, and the bases need not be aligned to 16 bytes
+    y, h = oc.rms_norm(x.cuda(), w.cuda(), residual=r.cuda(), eps=EPS, out_dtype=ot)
+    H = x.double() + r.double()
+    near(h, H, UNIT[st] * H.abs() + U32 * H.abs() + TINY[st], "h")
+    want, _ = norm_reference(H, w.double())
+    rel = UNIT[ot] + (c + 24) * U32
+    # the sum's own rounding to float reaches y at its full size
+    near(y, want, rel * want.abs() + TINY[ot], "y")
+    y1, h1 = oc.rms_norm(x.cuda(), w.cuda(), eps=EPS, out_dtype=ot)
+    want, _ = norm_reference(x.double(), w.double())
+    near(y1, want, rel * want.abs() + TINY[ot], "y without residual")
+    assert h1.shape == x.shape
+
+
+def test_norm_unaligned_base():
+    from paper_1611_05009_amd import octnet as oc
+    flat = randn(3, 1 + 40 * 64).to(torch.bfloat16).cuda()
+    w = (1 + 0.1 * randn(4, 64)).cuda()
+    a, _ = oc.rms_norm(flat[1:].view(40, 64), w)
+    b, _ = oc.rms_norm(flat[1:].view(40, 64).clone(), w)
+    near(a, b.cpu().double(), 2 * UNIT[torch.bfloat16] * b.cpu().double().abs(), "unaligned")
+
+
+@pytest.mark.parametrize("dt", TYPES, ids=str)
+@pytest.mark.parametrize("c", [5, 64, 1000, 4096, 9001])
+def test_norm_8bit(c, dt):
+    """The 8-bit value is the nearest to y / scale, or its neighbour where
+    y / scale lies within the float computation's error of the middle."""
+    from paper_1611_05009_amd import octnet as oc
+    x, r, w = norm_inputs(33, c, dt, dt)
+    y, scale, h = oc.rms_norm_8bit(x.cuda(), w.cuda(), residual=r.cuda(), eps=EPS)
+    want, _ = norm_reference(x.double() + r.double(), w.double())
+    rel = (c + 32) * U32
+    most = want.abs().amax(1)
+    near(scale, torch.where(most > 0, most / 448, torch.ones_like(most)), rel * most / 448 + 0.0, "scale")
+    t = want / scale.cpu().double()[:, None]
+    step = torch.exp2(torch.floor(torch.log2(t.abs().clamp(min=2.0 ** -6))) - 3)
+    # half a step; the step of the binade above at its lower edge
+    near(y.float(), t, step * 0.5 * (1 + 1e-12) + rel * t.abs() + 2.0 ** -60, "y")
+    assert not y[2].float().any() and float(scale[2]) == 1.0
+
+
+@pytest.mark.parametrize("st,dt", [(torch.float32, torch.float32), (torch.bfloat16, torch.bfloat16),
+                                   (torch.float32, torch.bfloat16), (torch.float16, torch.float16)])
+@pytest.mark.parametrize("rows,c", [(1, 8), (67, 17), (1000, 64), (300, 100), (131, 513), (77, 1000), (50, 2056), (9, 9001),
+                                    (5000, 3), (20000, 32)])
+def test_norm_backward(rows, c, st, dt):
+    from paper_1611_05009_amd import octnet as oc
+    h, dy, ds = (1.5 * randn(c, rows, c)).to(st), randn(c + 1, rows, c).to(dt), randn(c + 2, rows, c).to(st)
+    w = 1 + 0.3 * randn(c + 3, c)
+    H, D, W = h.double(), dy.double(), w.double()
+    rms = (H.square().mean(1, keepdim=True) + EPS).sqrt()
+    n, u = H / rms, D * W
+    dot = (u * n).mean(1, keepdim=True)
+    size = ((u - n * dot) / rms)
+    mag = (u.abs() + n.abs() * (u * n).abs().mean(1, keepdim=True)) / rms
+    rel = (c + 32) * U32
+    for extra in (ds, None):
+        dx, dw = oc.rms_norm_backward(h.cuda(), w.cuda(), dy.cuda(), dsum=None if extra is None else extra.cuda(), eps=EPS)
+        want = size + (extra.double() if extra is not None else 0)
+        near(dx, want, UNIT[st] * want.abs() + rel * mag + 2 * U32 * want.abs() + TINY[st], "dx")
+        near(dw, (D * n).sum(0), (c + rows + 32) * U32 * (D * n).abs().sum(0), "dweight")
+    dx2, none = oc.rms_norm_backward(h.cuda(), w.cuda(), dy.cuda(), eps=EPS, need_weight=False)
+    assert none is None and torch.equal(dx2, dx)
+
+
+def test_norm_backward_against_differences():
+    """Central differences of sum(y dy) in 64 bits; their error is of order
+    t^2 = 1e-10 of the third derivative, the gradients' that of float."""
+    from paper_1611_05009_amd import octnet as oc
+    rows, c, t = 40, 96, 1e-5
+    h, dy, w = randn(1, rows, c), randn(2, rows, c), 1 + 0.3 * randn(3, c)
+    dx, dw = oc.rms_norm_backward(h.cuda(), w.cuda(), dy.cuda(), eps=EPS)
+    a, b = randn(4, rows, c).double(), randn(5, c).double()
+    loss = lambda s: float((norm_reference(h.double() + s * t * a, w.double() + s * t * b)[0] * dy.double()).sum())  # noqa: E731
+    want = (loss(1) - loss(-1)) / (2 * t)
+    got = float((dx.cpu().double() * a).sum() + (dw.cpu().double() * b).sum())
+    assert abs(got - want) <= 1e-5 * float((dx.cpu().double() * a).abs().sum() + (dw.cpu().double() * b).abs().sum())
+
+
+def test_norm_without_rows():
+    from paper_1611_05009_amd import octnet as oc
+    w = torch.ones(16, device="cuda")
+    x = torch.empty((0, 16), device="cuda")
+    assert oc.rms_norm(x, w)[0].shape == (0, 16)
+    dx, dw = oc.rms_norm_backward(x, w, x)
+    assert dx.shape == (0, 16) and not dw.any()
+
+
+# ---------------------------------------------------------------------------
+# Labels
+# ---------------------------------------------------------------------------
+
+
+def label_inputs(seed, rows, classes, dtype, masked, ties=False):
+    g = torch.Generator().manual_seed(seed)
+    x = 3 * torch.randn((rows, classes), generator=g)
+    if ties:
+        x = x.round()
+    x[torch.rand((rows, classes), generator=g) < masked] = -math.inf
+    labels = torch.randint(-1, classes, (rows,), generator=g, dtype=torch.int32)
+    if rows > 4:
+        x[3] = -math.inf        # a row without any class
+        x[4] = 0.25             # all equal
+    return x.to(dtype), labels
+
+
+def label_reference(x, labels, top):
+    x = x.double()
+    lse = torch.logsumexp(x, 1)
+    none = lse == -math.inf
+    lp = torch.where(none[:, None], torch.tensor(-math.inf, dtype=torch.float64), x - torch.where(none, 0.0, lse)[:, None])
+    ent = torch.special.entr(lp.exp()).sum(1)
+    has = (labels >= 0) & (labels < x.shape[1])
+    mine = lp.gather(1, torch.where(has, labels, 0).long()[:, None])[:, 0]
+    order = torch.sort(x, dim=1, descending=True, stable=True).indices[:, :top]
+    return lse, torch.where(has, mine, 0.0), ent, order, lp
+
+
+def check_labels(x, labels, top, seed=0):
+    from paper_1611_05009_amd import octnet as oc
+    rows, classes = x.shape
+    a = oc.label_logprobs(x.cuda(), labels.cuda(), top=top)
+    lse, mine, ent, order, lp = label_reference(x, labels, top)
+    big = torch.where(torch.isfinite(x.double()), x.double().abs(), 0.0).amax(1)
+    rel = (classes + 16 + 4 * big) * U32           # of the sum of exponentials
+    bar = rel + 4 * U32 * (1 + big + lse.abs().nan_to_num(posinf=0, neginf=0))
+    near(a.lse, lse, bar, "lse")
+    near(a.logprob, mine, bar + 2 * U32 * mine.abs().nan_to_num(posinf=0, neginf=0), "logprob")
+    p = lp.exp()
+    zmax = torch.where(p > 0, lp.abs(), 0.0).amax(1)
+    e_ent = rel * (2 + 2 * ent + (p * torch.where(p > 0, lp.abs(), 0.0)).sum(1)) + 8 * U32 * (1 + zmax)
+    near(a.entropy, ent, e_ent, "entropy")
+    if top:
+        assert torch.equal(a.top_label.cpu().long(), order), "top labels"
+        want = lp.gather(1, order)
+        near(a.top_logprob, want, (bar[:, None] + 2 * U32 * want.abs().nan_to_num(posinf=0, neginf=0)), "top logprob")
+    g, ge = randn(seed + 1, rows), randn(seed + 2, rows)
+    has = (labels >= 0) & (labels < classes) & (lse > -math.inf)
+    G = torch.where(has, g.double(), 0.0)
+    hit = torch.zeros_like(p)
+    hit[torch.arange(rows), torch.where(has, labels, 0).long()] = 1.0
+    for e in (ge, None):
+        d = oc.label_logprobs_backward(x.cuda(), labels.cuda(), a.lse, g.cuda(), entropy=a.entropy,
+                                       dentropy=None if e is None else e.cuda())
+        E = 0.0 if e is None else e.double()[:, None]
+        want = G[:, None] * (hit * has[:, None] - p) + E * (torch.special.entr(p) - p * ent[:, None])
+        size = p * (G.abs()[:, None] + (0.0 if e is None else E.abs() * (torch.where(p > 0, lp.abs(), 0.0) + ent[:, None])))
+        ep = bar[:, None] + 4 * U32 * (2 + torch.where(p > 0, lp.abs(), 0.0))
+        u = UNIT[x.dtype]
+        lim = u * want.abs() + size * ep + (0.0 if e is None else p * E.abs() * (bar + e_ent)[:, None]) \
+            + 4 * U32 * (size + G.abs()[:, None] * hit) + TINY[x.dtype]
+        near(d, want, lim, "dlogits")
+    y = x.cuda()
+    b = oc.label_logprobs_backward(y, labels.cuda(), a.lse, g.cuda(), out=y)
+    assert b is y and torch.equal(y, d)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("rows,classes,top,masked", [(1, 1, 1, 0.0), (500, 2, 2, 0.0), (300, 8, 3, 0.2), (77, 13, 13, 0.5),
+                                                     (65, 64, 4, 0.0), (33, 512, 32, 0.1), (20, 517, 5, 0.9), (9, 2048, 8, 0.0),
+                                                     (7, 2049, 8, 0.0), (6, 5003, 32, 0.1), (5, 30011, 20, 0.99),
+                                                     (700, 2100, 3, 0.0), (1300, 4097, 1, 0.05)])
+def test_labels(rows, classes, top, masked, dtype):
+    x, labels = label_inputs(rows + classes, rows, classes, dtype, masked)
+    check_labels(x, labels, top)
+
+
+@pytest.mark.parametrize("classes", [40, 1500, 20001])
+def test_labels_with_ties(classes):
+    """Many equal logits: the top entries go by index."""
+    x, labels = label_inputs(5, 40, classes, torch.bfloat16, 0.1, ties=True)
+    check_labels(x, labels, min(32, classes))
+
+
+@pytest.mark.parametrize("order", ["up", "down"])
+def test_labels_in_order(order):
+    """Ascending logits enter the lists at every step, descending ones never."""
+    x = torch.linspace(-20, 20, 50001).expand(3, -1).contiguous()
+    x = x if order == "up" else x.flip(1).contiguous()
+    check_labels(x, torch.tensor([0, 50000, -1], dtype=torch.int32), 32)
+
+
+def test_labels_few_left():
+    """Fewer classes left than alternatives asked for: ruled-out ones follow in
+    order.  A NaN shows in the statistics and is no alternative."""
+    from paper_1611_05009_amd import octnet as oc
+    for classes in (40, 9000):
+        x = torch.full((3, classes), -math.inf)
+        x[0, 7], x[0, 3] = 1.0, 2.0
+        x[1, classes - 1] = 0.0
+        x[2] = 0.0
+        x[2, 5] = math.nan
+        a = oc.label_logprobs(x.cuda(), torch.tensor([3, 0, 1], dtype=torch.int32).cuda(), top=4)
+        assert a.top_label.cpu().tolist() == [[3, 7, 0, 1], [classes - 1, 0, 1, 2], [0, 1, 2, 3]]
+        assert a.top_logprob[0, 2:].cpu().tolist() == [-math.inf] * 2
+        assert math.isnan(a.lse[2]) and math.isnan(a.logprob[2]) and math.isnan(a.entropy[2])
+        assert float(a.logprob[1]) == -math.inf and float(a.entropy[1]) == 0.0
+    b = oc.label_logprobs(x.cuda(), torch.tensor([3, 9000, -5], dtype=torch.int32).cuda(), entropy=False)
+    assert b.entropy is None and float(b.logprob[1]) == 0.0 and float(b.logprob[2]) == 0.0
+
+
+def test_labels_gradient_against_differences():
+    """Central differences of the 64-bit loss along a direction; error of
+    order t^2 = 1e-10, gradients in float."""
+    from paper_1611_05009_amd import octnet as oc
+    rows, classes, t = 30, 50, 1e-5
+    x, labels = randn(1, rows, classes), torch.randint(-1, classes, (rows,), generator=torch.Generator().manual_seed(2),
+                                                       dtype=torch.int32)
+    g, ge, way = randn(3, rows), randn(4, rows), randn(5, rows, classes).double()
+    a = oc.label_logprobs(x.cuda(), labels.cuda())
+    d = oc.label_logprobs_backward(x.cuda(), labels.cuda(), a.lse, g.cuda(), entropy=a.entropy, dentropy=ge.cuda())
+
+    def loss(s):
+        _, mine, ent, _, _ = label_reference(x.double() + s * t * way, labels, 1)
+        return float((mine * g.double()).sum() + (ent * ge.double()).sum())
+
+    want = (loss(1) - loss(-1)) / (2 * t)
+    got = float((d.cpu().double() * way).sum())
+    assert abs(got - want) <= 1e-5 * float((d.cpu().double() * way).abs().sum())
+
+
+# ---------------------------------------------------------------------------
+# Clipping
+# ---------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("seed,n,dtypes", [(0, 1, TYPES[:1]), (1, 7, TYPES), (2, 300, TYPES), (3, 40, TYPES[2:])])
+@pytest.mark.parametrize("clip", [True, False])
+def test_clip(seed, n, dtypes, clip):
+    from paper_1611_05009_amd import octnet as oc
+    rng = np.random.default_rng(seed)
+    grads = []
+    for i in range(n):
+        size = int(rng.integers(0, 20)) if i % 3 == 0 else int(rng.integers(1, 70000))
+        t = (0.02 * torch.randn(size + 1, generator=torch.Generator().manual_seed(100 * seed + i))).to(dtypes[i % len(dtypes)]).cuda()
+        grads.append(t[1:] if i % 4 == 1 else t[:-1])     # some not aligned to 16 bytes
+    flat = [t.cpu().double() for t in grads]
+    norm = math.sqrt(sum(float(t.square().sum()) for t in flat))
+    most = norm * (0.3 if clip else 2.0)
+    f = min(1.0, most / (norm + 1e-6))
+    out = [torch.full_like(t, 7.0) for t in grads]
+    got = oc.clip_grad_norm(grads, most, out=out)
+    # double sums: the float result is the nearest, or beside it
+    assert abs(float(got) - norm) <= 2 * U32 * norm
+    for t, o, x in zip(flat, out, grads):
+        near(o, t * f, (UNIT[x.dtype] + 3 * U32) * (t * f).abs() + TINY[x.dtype], "out %d" % t.numel())
+        assert torch.equal(x.cpu().double(), t)
+    same = [t.clone() for t in grads]
+    again = oc.clip_grad_norm(same, most)
+    assert torch.equal(again, got) and all(torch.equal(a, b) for a, b in zip(same, out))
+
+
+def test_clip_extremes():
+    from paper_1611_05009_amd import octnet as oc
+    assert float(oc.clip_grad_norm([], 1.0)) == 0.0
+    e = torch.empty(0, device="cuda")
+    assert float(oc.clip_grad_norm([e, e], 1.0)) == 0.0
+    # squares beyond float
+    t = torch.full((1000,), 1e30, device="cuda")
+    norm = oc.clip_grad_norm([t], 1.0)
+    assert abs(float(norm) / (1e30 * math.sqrt(1000)) - 1) < 1e-6
+    assert torch.allclose(t, torch.full_like(t, 1 / math.sqrt(1000)), rtol=1e-6)
+    t = torch.tensor([1.0, math.inf], device="cuda")
+    assert math.isinf(float(oc.clip_grad_norm([t], 1.0))) and float(t[0]) == 0.0 and math.isnan(t[1])
+    t = torch.tensor([1.0, math.nan], device="cuda")
+    assert math.isnan(float(oc.clip_grad_norm([t], 1.0))) and math.isnan(t[0])
+    z = torch.zeros(5, device="cuda")
+    assert float(oc.clip_grad_norm([z], 0.0)) == 0.0 and not z.any()
+
+
+def test_row_operators_in_a_graph():
+    """Recorded once and replayed on new contents, against eager calls."""
+    from paper_1611_05009_amd import octnet as oc
+    x, w = torch.randn(300, 72, device="cuda"), torch.rand(72, device="cuda") + 0.5
+    labels = torch.randint(0, 72, (300,), dtype=torch.int32, device="cuda")
+    dy = torch.randn_like(x)
+
+    def step():
+        y, _ = oc.rms_norm(x, w)
+        a = oc.label_logprobs(y, labels, top=2)
+        d = oc.label_logprobs_backward(y, labels, a.lse, dy[:, 0].contiguous())
+        dx, dw = oc.rms_norm_backward(x, w, d)
+        q = x.view(300, 9, 8)
+        o, lse = oc.attention(q, q[:, :3], q[:, 3:6], causal=True)
+        gq, gk, gv = oc.attention_backward(q, q[:, :3], q[:, 3:6], o, lse, o, causal=True)
+        out = [torch.empty_like(t) for t in (dx, dw, gq)]
+        return [y, a.logprob, a.top_label, dx, dw, o, gk, gv, oc.clip_grad_norm([dx, dw, gq], 0.1, out=out)] + out
+
+    step()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        kept = step()
+    for k in range(3):
+        x.copy_(torch.randn(x.shape, generator=torch.Generator().manual_seed(k)))
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(kept, step()))
+        torch.cuda.synchronize()
