@@ -505,8 +505,9 @@ int oc_points_vote(const int32_t* rows, int64_t n_pts, const int32_t* labels, in
  *   multiple of kv_heads, scale positive.
  *   q_off, k_off: int64 [n_seq + 1], sequence s has query rows
  *   q_off[s] .. q_off[s + 1] - 1 and key rows k_off[s] ..; they start at 0,
- *   end at n_q and n_k and do not decrease (values outside are clamped; rows
- *   of no sequence are not written).  NULL (n_seq 1): one sequence.
+ *   end at n_q and n_k and do not decrease (values outside are clamped; the
+ *   outputs of rows of no sequence are undefined).  NULL (n_seq 1): one
+ *   sequence.
  *   k_len: int64 [n_seq], the keys of sequence s are the first k_len[s] rows
  *   of its range (a cache that is filled in part); NULL: all of it.
  *   out: [n_q][heads][dim] of type dtype, lse: float [n_q][heads].

@@ -682,7 +682,10 @@ int attention_args(const char* who, const void* q, int64_t q_row, int64_t q_head
   if (!(scale > 0.f) || !isfinite(scale)) return fail(OC_EINVAL, "%s: scale %g is not positive", who, scale);
   const int64_t strides[] = {q_row, q_head, k_row, k_head, v_row, v_head};
   for (int64_t x : strides)
-    if (x < 0 || x * type_bytes(dtype) % 16) return fail(OC_EINVAL, "%s: stride %lld is no multiple of 16 bytes", who, (long long)x);
+    if (x < 0 || x >= (1LL << 40) || x * type_bytes(dtype) % 16)
+      return fail(OC_EINVAL, "%s: stride %lld is negative, too large or no multiple of 16 bytes", who, (long long)x);
+  // The gradient forms a query's place from 32-bit factors.
+  if (q_row >= (1LL << 32) || q_head >= (1LL << 32)) return fail(OC_EOVERFLOW, "%s: query strides >= 2^32", who);
   if (!aligned16(q) || !aligned16(k) || !aligned16(v)) return fail(OC_EINVAL, "%s: pointer not aligned to 16 bytes", who);
   *a = oci::AttnArgs();
   a->q = q; a->k = k; a->v = v;
@@ -744,7 +747,8 @@ int oc_attention_backward_workspace(int64_t n_q, int64_t n_k, int n_seq, int hea
   if (!bytes) return fail(OC_EINVAL, "oc_attention_backward_workspace: null pointer");
   const int rc = attention_sizes("oc_attention_backward_workspace", n_q, n_k, n_seq, heads, kv_heads, dim);
   if (rc != OC_OK) return rc;
-  *bytes = 2 * oci::align256(4 * (size_t)n_q * heads);
+  *bytes = 2 * oci::align256(4 * (size_t)n_q * heads) +
+           oci::attention_back_parts(n_q, n_k, n_seq, heads, kv_heads, dim).bytes;
   return OC_OK;
 }
 
@@ -764,7 +768,8 @@ int oc_attention_backward(const void* q, int64_t q_row, int64_t q_head, const vo
   if (!aligned16(out) || !aligned16(dout) || !aligned16(dq) || !aligned16(dk) || !aligned16(dv))
     return fail(OC_EINVAL, "oc_attention_backward: pointer not aligned to 16 bytes");
   const size_t part = oci::align256(4 * (size_t)n_q * heads);
-  if (n_q > 0 && (!ws || ws_bytes < 2 * part)) return fail(OC_EWORKSPACE, "oc_attention_backward: workspace too small");
+  const size_t need = 2 * part + oci::attention_back_parts(n_q, n_k, n_seq, heads, kv_heads, dim).bytes;
+  if (need && (!ws || ws_bytes < need)) return fail(OC_EWORKSPACE, "oc_attention_backward: workspace too small");
   if (!aligned16(ws)) return fail(OC_EINVAL, "oc_attention_backward: workspace not aligned to 16 bytes");
   a.out = const_cast<void*>(out);
   a.lse = const_cast<float*>(lse);
@@ -772,6 +777,7 @@ int oc_attention_backward(const void* q, int64_t q_row, int64_t q_head, const vo
   a.dq = dq; a.dk = dk; a.dv = dv;
   a.delta = static_cast<float*>(ws);
   a.lse2 = reinterpret_cast<float*>(static_cast<char*>(ws) + part);
+  a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + 2 * part);
   OC_CHECK_HIP(oci::launch_attention_backward(a, dtype, as_stream(stream)), "oc_attention_backward");
   return OC_OK;
 }

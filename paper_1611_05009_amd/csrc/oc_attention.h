@@ -18,7 +18,8 @@ struct AttnArgs {
   int causal;
   void* out;                             // [n_q][heads][dim]
   float* lse;                            // [n_q][heads]
-  // Forward with split keys: parts [n_split][n_q][heads](...)
+  // Split keys (forward, dq: parts [n_split][n_q][heads](...)) or rows
+  // (dk and dv: parts [n_split][2][n_k][kv_heads][dim])
   int n_split;
   float *part, *part_lse;
   // Backward
@@ -32,6 +33,12 @@ void attention_set_group(AttnArgs* a);
 // Parts into which the keys of each row tile are split.
 int attention_splits(int64_t n_q, int64_t n_k, int n_seq, int heads, int kv_heads);
 hipError_t launch_attention(const AttnArgs& a, int dtype, hipStream_t s);
-hipError_t launch_attention_backward(const AttnArgs& a, int dtype, hipStream_t s);
+// Parts of the gradients' kernels and the bytes that these take.
+struct AttnParts {
+  int dq, dkv;
+  size_t bytes;
+};
+AttnParts attention_back_parts(int64_t n_q, int64_t n_k, int n_seq, int heads, int kv_heads, int dim);
+hipError_t launch_attention_backward(AttnArgs a, int dtype, hipStream_t s);
 
 }  // namespace oci

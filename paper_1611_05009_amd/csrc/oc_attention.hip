@@ -158,34 +158,69 @@ struct Tile {
   }
 };
 
-// Copy of a tile from global memory through registers: load() issues the
-// reads, store() writes them to LDS.  Rows past the end and columns past the
-// head size become zero, whatever lies there in memory.
+// n / d for n < 2^31 (AttnArgs::div_*).
+__device__ __forceinline__ int by_group(const AttnArgs& a, int n) {
+  return (int)((__umulhi(a.div_mul, (uint32_t)n) + (uint32_t)n) >> a.div_shift);
+}
+
+// Rows past the end and columns past the head size are copied from here.
+__device__ const u32x4 kZeros = {0, 0, 0, 0};
+
+// Copy of tiles from global memory straight into LDS.  A wave's 64 chunks land
+// one after the other, so the chunk that belongs at a position is what each
+// lane asks for.  A copy is asynchronous until the next wait_copies().
 template <class T, int D, int R, int NT>
 struct Stage {
   using L = Tile<T, D, R>;
-  static constexpr int kN = (R * L::kChunks + NT - 1) / NT;
-  u32x4 x[kN];
+  static constexpr int kN = R * L::kChunks / NT;    // chunks per thread
+  static constexpr int kStep = NT / L::kChunks;     // rows between them
+  static_assert(R * L::kChunks % NT == 0 && kStep % 8 == 0, "whole waves, one swizzle per thread");
 
-  // row_at(r): the address of row r's first element, or null.
-  template <class F>
-  __device__ __forceinline__ void load(int dim, F row_at) {
+  int row, col;   // the thread's first row, and its column, in the tile
+  __device__ __forceinline__ Stage() {
+    row = (int)threadIdx.x / L::kChunks;
+    col = (((int)threadIdx.x % L::kChunks) ^ L::swizzle(row)) * L::kPer;
+  }
+
+  static __device__ __forceinline__ void put(char* t, int i, const void* p) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p,
+                                     (__attribute__((address_space(3))) void*)(t + (wave() * 64 + i * NT) * 16), 16, 0, 0);
+  }
+
+  // R rows from p on, `stride` elements apart, of which `rows` exist.
+  __device__ __forceinline__ void copy(char* t, const T* p, int64_t stride, int rows, int dim) const {
+    const T* q = p + row * stride + col;
+    if (rows >= R && dim == D) {
 #pragma unroll
-    for (int i = 0; i < kN; ++i) {
-      const int n = (int)threadIdx.x + i * NT;
-      const int r = n / L::kChunks, c = (n % L::kChunks) ^ L::swizzle(r);
-      const T* p = (R * L::kChunks % NT == 0 || r < R) && c * L::kPer < dim ? row_at(r) : nullptr;
-      x[i] = p ? *(const u32x4*)(p + c * L::kPer) : u32x4{0, 0, 0, 0};
+      for (int i = 0; i < kN; ++i) put(t, i, q + i * kStep * stride);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kN; ++i) {
+        const bool in = (col < dim) & (row + i * kStep < rows);
+        put(t, i, in ? (const void*)(q + i * kStep * stride) : (const void*)&kZeros);
+      }
     }
   }
-  __device__ __forceinline__ void store(char* t) const {
+
+  // Packed rows r .. r + R - 1 of two arrays, of which those below `rows`
+  // exist; offset_x and offset_y map (query, head of the group) to elements.
+  template <class A, class X, class Y>
+  __device__ __forceinline__ void copy_packed(char* tx, char* ty, const A& a, int r, int rows, X at_x, Y at_y) const {
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
-      const int n = (int)threadIdx.x + i * NT;
-      if (R * L::kChunks % NT == 0 || n < R * L::kChunks) *(u32x4*)(t + n * 16) = x[i];
+      const int n = r + row + i * kStep;
+      const bool in = (col < a.dim) & (n < rows);
+      const int q = by_group(a, n), g = n - q * a.group;
+      put(tx, i, in ? (const void*)(at_x(q, g) + col) : (const void*)&kZeros);
+      put(ty, i, in ? (const void*)(at_y(q, g) + col) : (const void*)&kZeros);
     }
   }
 };
+
+__device__ __forceinline__ void wait_copies() {
+  __builtin_amdgcn_s_waitcnt(0x0f70);  // vector memory only
+  __syncthreads();
+}
 
 // ---------------------------------------------------------------------------
 // Sequences and tiles
@@ -195,11 +230,6 @@ struct Seq {
   int64_t q0, k0;  // first query and key row
   int lq, lk;      // queries and keys
 };
-
-// n / d for n < 2^31 (AttnArgs::div_*).
-__device__ __forceinline__ int by_group(const AttnArgs& a, int n) {
-  return (int)((__umulhi(a.div_mul, (uint32_t)n) + (uint32_t)n) >> a.div_shift);
-}
 
 // Offsets come from device memory, unchecked: clamped into the arrays, so
 // that wrong ones give wrong results and no access outside.
@@ -218,23 +248,71 @@ __device__ __forceinline__ Seq seq_of(const AttnArgs& a, int s) {
   return e;
 }
 
-// Tiles of sequences whose lengths only the device knows: sequence s with
-// first row o owns slots o / tile + s onwards, which leaves room for
-// ceil(length / tile) tiles whatever the lengths.  Returns the sequence of
-// `slot` (64 candidates per step), and its first slot.
-__device__ __forceinline__ int seq_of_slot(const int64_t* off, int n_seq, int64_t n, int mul, int tile, int64_t slot,
-                                           int64_t* first) {
-  if (!off) {
-    *first = 0;
-    return 0;
+// One tile of `tile` rows of one sequence.
+struct Place {
+  int s;     // sequence, negative: none
+  int at;    // the tile's number in it
+  int n;     // tiles of the sequence (0: not known)
+};
+
+// The x-th tile of sequences whose lengths only the device knows, from
+// rows / tile + n_seq numbers (an upper bound of all tiles; the rest find
+// none).  Up to 64 sequences, one per lane: tiles are counted by their number
+// in their sequence, greatest numbers first, so that the tiles with the most
+// work start first however lengths are mixed.  Sum over sequences of max(0, n
+// - l) tiles have number l or greater; l is found by bisection.  More
+// sequences: sequence s owns the numbers from first row / tile + s on, which
+// leaves room for its tiles whatever the lengths.
+__device__ __forceinline__ Place place_of(const int64_t* off, int n_seq, int64_t rows, int mul, int tile, int64_t x,
+                                          int64_t numbers) {
+  Place p{-1, 0, 0};
+  if (n_seq <= 64) {
+    int n = 0;
+    if (!off) {
+      n = lane() == 0 ? (int)((rows * mul + tile - 1) / tile) : 0;
+    } else if (lane() < n_seq) {
+      const int64_t a = bounded(off[lane()], 0, rows), b = bounded(off[lane() + 1], a, rows);
+      n = (int)(((b - a) * mul + tile - 1) / tile);
+    }
+    int hi = n;  // one past the greatest number
+#pragma unroll
+    for (int i = 32; i; i >>= 1) {
+      const int o = __shfl_xor(hi, i);
+      hi = o > hi ? o : hi;
+    }
+    hi = __builtin_amdgcn_readfirstlane(hi);
+    // Least l of which at most x tiles have greater numbers.
+    int lo = 0, above = 0;
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      int more = n > mid + 1 ? n - mid - 1 : 0;
+#pragma unroll
+      for (int i = 32; i; i >>= 1) more += __shfl_xor(more, i);
+      more = __builtin_amdgcn_readfirstlane(more);
+      if (more <= x) {
+        hi = mid;
+        above = more;
+      } else {
+        lo = mid + 1;
+      }
+    }
+    uint64_t have = __ballot(n > lo);
+    int skip = (int)(x - above);
+    if (x - above >= __popcll(have)) return p;
+    for (; skip > 0; --skip) have &= have - 1;
+    p.s = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)have) - 1);
+    p.at = lo;
+    p.n = __builtin_amdgcn_readlane(n, p.s);
+    return p;
   }
-  int lo = 0, count = n_seq;  // the answer lies in [lo, lo + count)
+  x = numbers - 1 - x;
+  int lo = 0, count = n_seq;  // the answer lies in [lo, lo + count), 64 candidates per step
   while (count > 1) {
     const int step = (count + 63) / 64;
     const int s = lo + lane() * step;
     const bool in = s < lo + count;
-    const int64_t start = in ? bounded(off[s], 0, n) * mul / tile + s : 0;
-    const int hits = __popcll(__ballot(in && start <= slot));
+    const int64_t start = in ? bounded(off[s], 0, rows) * mul / tile + s : 0;
+    const int hits = __popcll(__ballot(in && start <= x));
     // Candidate 0 always qualifies for lo = 0; keep lo if offsets are wrong.
     const int k = hits > 0 ? hits - 1 : 0;
     const int left = count - k * step;
@@ -242,8 +320,11 @@ __device__ __forceinline__ int seq_of_slot(const int64_t* off, int n_seq, int64_
     count = left < step ? left : step;
   }
   lo = __builtin_amdgcn_readfirstlane(lo);
-  *first = bounded(off[lo], 0, n) * mul / tile + lo;
-  return lo;
+  const int64_t at = x - (bounded(off[lo], 0, rows) * mul / tile + lo);
+  if (at < 0 || at >= numbers) return p;
+  p.s = lo;
+  p.at = __builtin_amdgcn_readfirstlane((int)at);
+  return p;
 }
 
 // Keys that packed row r of the sequence sees: the first `seen` ones.
@@ -296,27 +377,43 @@ __device__ __forceinline__ void store_col(T* p, const f32x16& c, int d0, int dim
   }
 }
 
+// Step sizes and waves per SIMD by type and head size.  Two waves of a SIMD
+// cover each other's softmax and LDS reads: at head size 128 in bfloat16 the
+// forward pass measured 488 TFLOP/s with one and 727 with two.  The steps are the
+// largest whose two buffers leave LDS, and whose fragments leave registers, for
+// the second wave; dK and dV at head sizes over 64 also need the values in LDS
+// instead of registers for that (503 to 774 TFLOP/s).  32-bit fragments are
+// twice as large and leave room for one wave in the gradients.
+template <class T, int D>
+struct Plan {
+  static constexpr bool kWide = D > 64, kHalf = sizeof(T) == 2;
+  static constexpr int kKeys = kHalf || !kWide ? 64 : 32;       // forward
+  static constexpr int kDqKeys = kHalf ? 64 : 32;
+  static constexpr int kDqWaves = kHalf || !kWide ? 2 : 1;
+  static constexpr int kDkvRows = kHalf && !kWide ? 64 : 32;
+  static constexpr int kDkvWaves = kHalf || D <= 32 ? 2 : 1;
+  static constexpr bool kValuesInLds = kHalf && kWide;
+};
+
 // ---------------------------------------------------------------------------
 // Forward
 // ---------------------------------------------------------------------------
 
 // NW waves of MT x 32 packed rows each, BN keys per step, two LDS buffers.
 template <class T, int D, int MT, int NW, int BN>
-__global__ __launch_bounds__(NW * 64) void k_attention(AttnArgs a) {
+__global__ __launch_bounds__(NW * 64, 2) void k_attention(AttnArgs a) {
   using L = Tile<T, D, BN>;
   constexpr int NT = NW * 64, BM = NW * MT * 32;
   __shared__ __attribute__((aligned(16))) char lds[2][2][L::kBytes];
 
   const int kvh = (int)(blockIdx.x % (unsigned)a.kv_heads);
-  // Rows with the most keys first where the mask is causal.
-  const int64_t slot = (int64_t)(gridDim.x / (unsigned)a.kv_heads) - 1 - blockIdx.x / (unsigned)a.kv_heads;
-  int64_t first;
-  const int s = seq_of_slot(a.q_off, a.n_seq, a.n_q, a.group, BM, slot, &first);
-  const Seq e = seq_of(a, s);
+  const Place p = place_of(a.q_off, a.n_seq, a.n_q, a.group, BM, blockIdx.x / (unsigned)a.kv_heads,
+                           gridDim.x / (unsigned)a.kv_heads);
+  if (p.s < 0) return;
+  const Seq e = seq_of(a, p.s);
   const int rows = e.lq * a.group;
-  const int64_t r0_64 = (slot - first) * BM;
-  if (r0_64 < 0 || r0_64 >= rows) return;
-  const int r0 = (int)r0_64;
+  if ((int64_t)p.at * BM >= rows) return;
+  const int r0 = p.at * BM;
 
   const int w = wave(), l32 = lane() & 31, h = lane() >> 5;
   // Keys of this tile, and of this part where the keys are split.
@@ -342,9 +439,9 @@ __global__ __launch_bounds__(NW * 64) void k_attention(AttnArgs a) {
     const int rr = r < rows ? r : rows - 1;
     seen[m] = seen_keys(a, e, rr);
     seen_min[m] = __builtin_amdgcn_readfirstlane(seen_keys(a, e, w0 < rows ? w0 : rows - 1));
-    const T* p = q + row_offset(a, rr, a.q_row, a.q_head);
+    const T* qp = q + row_offset(a, rr, a.q_row, a.q_head);
 #pragma unroll
-    for (int i = 0; i < D / 16; ++i) qf[m][i] = global_frag<T>(p, true, 16 * i, a.dim);
+    for (int i = 0; i < D / 16; ++i) qf[m][i] = global_frag<T>(qp, true, 16 * i, a.dim);
     const int e1 = w0 + 31 < rows ? w0 + 31 : rows - 1;
     const int mx = w0 < rows ? seen_keys(a, e, e1) : 0;
     seen_max = mx > seen_max ? mx : seen_max;
@@ -362,21 +459,18 @@ __global__ __launch_bounds__(NW * 64) void k_attention(AttnArgs a) {
   }
   const float c = a.scale * kLog2e;
 
-  Stage<T, D, BN, NT> ks, vs;
-  const auto load = [&](int t) {
-    ks.load(a.dim, [&](int r) { return t * BN + r < e.lk ? k + (int64_t)(t * BN + r) * a.k_row : nullptr; });
-    vs.load(a.dim, [&](int r) { return t * BN + r < e.lk ? v + (int64_t)(t * BN + r) * a.v_row : nullptr; });
+  const Stage<T, D, BN, NT> stage;
+  const auto load = [&](int t, int b) {
+    const int64_t j = (int64_t)t * BN;
+    stage.copy(lds[b][0], k + j * a.k_row, a.k_row, e.lk - (int)j, a.dim);
+    stage.copy(lds[b][1], v + j * a.v_row, a.v_row, e.lk - (int)j, a.dim);
   };
-  if (t0 < t1) {
-    load(t0);
-    ks.store(lds[0][0]);
-    vs.store(lds[0][1]);
-  }
-  __syncthreads();
+  if (t0 < t1) load(t0, 0);
+  wait_copies();
   for (int t = t0; t < t1; ++t) {
     const char* kt = lds[(t - t0) & 1][0];
     const char* vt = lds[(t - t0) & 1][1];
-    if (t + 1 < t1) load(t + 1);
+    if (t + 1 < t1) load(t + 1, (t + 1 - t0) & 1);
     if (t * BN < seen_max) {
       f32x16 x[MT][BN / 32];
 #pragma unroll
@@ -443,11 +537,7 @@ __global__ __launch_bounds__(NW * 64) void k_attention(AttnArgs a) {
           }
         }
     }
-    if (t + 1 < t1) {
-      ks.store(lds[(t + 1 - t0) & 1][0]);
-      vs.store(lds[(t + 1 - t0) & 1][1]);
-    }
-    __syncthreads();
+    wait_copies();
   }
 
 #pragma unroll
@@ -526,22 +616,26 @@ __global__ __launch_bounds__(256) void k_attention_delta(AttnArgs a) {
 // dQ: waves of 32 packed rows over the keys, as the forward pass.
 //   S^T = K Q^T, dP^T = V dO^T, dS^T = P^T (dP^T - delta), dQ^T += K^T dS^T.
 template <class T, int D, int NW, int BN>
-__global__ __launch_bounds__(NW * 64) void k_attention_dq(AttnArgs a) {
+__global__ __launch_bounds__(NW * 64, (Plan<T, D>::kDqWaves)) void k_attention_dq(AttnArgs a) {
   using L = Tile<T, D, BN>;
   constexpr int NT = NW * 64, BM = NW * 32;
   __shared__ __attribute__((aligned(16))) char lds[2][2][L::kBytes];
   const int kvh = (int)(blockIdx.x % (unsigned)a.kv_heads);
-  const int64_t slot = (int64_t)(gridDim.x / (unsigned)a.kv_heads) - 1 - blockIdx.x / (unsigned)a.kv_heads;
-  int64_t first;
-  const int s = seq_of_slot(a.q_off, a.n_seq, a.n_q, a.group, BM, slot, &first);
-  const Seq e = seq_of(a, s);
+  const Place p = place_of(a.q_off, a.n_seq, a.n_q, a.group, BM, blockIdx.x / (unsigned)a.kv_heads,
+                           gridDim.x / (unsigned)a.kv_heads);
+  if (p.s < 0) return;
+  const Seq e = seq_of(a, p.s);
   const int rows = e.lq * a.group;
-  const int64_t r0_64 = (slot - first) * BM;
-  if (r0_64 < 0 || r0_64 >= rows) return;
-  const int r0 = (int)r0_64;
+  if ((int64_t)p.at * BM >= rows) return;
+  const int r0 = p.at * BM;
   const int w = wave(), l32 = lane() & 31, h = lane() >> 5;
   const int last = r0 + BM < rows ? r0 + BM - 1 : rows - 1;
-  const int t1 = (seen_keys(a, e, last) + BN - 1) / BN;
+  int t0 = 0, t1 = (seen_keys(a, e, last) + BN - 1) / BN;
+  if (a.n_split > 1) {
+    const int per = (t1 + a.n_split - 1) / a.n_split;
+    t0 = (int)blockIdx.y * per;
+    t1 = t0 + per < t1 ? t0 + per : t1;
+  }
 
   const T* q = (const T*)a.q + e.q0 * a.q_row + (int64_t)kvh * a.group * a.q_head;
   const T* k = (const T*)a.k + e.k0 * a.k_row + (int64_t)kvh * a.k_head;
@@ -568,21 +662,18 @@ __global__ __launch_bounds__(NW * 64) void k_attention_dq(AttnArgs a) {
   for (int d = 0; d < D / 32; ++d) g[d] = zero16();
   const float c = a.scale * kLog2e;
 
-  Stage<T, D, BN, NT> ks, vs;
-  const auto load = [&](int t) {
-    ks.load(a.dim, [&](int r) { return t * BN + r < e.lk ? k + (int64_t)(t * BN + r) * a.k_row : nullptr; });
-    vs.load(a.dim, [&](int r) { return t * BN + r < e.lk ? v + (int64_t)(t * BN + r) * a.v_row : nullptr; });
+  const Stage<T, D, BN, NT> stage;
+  const auto load = [&](int t, int b) {
+    const int64_t j = (int64_t)t * BN;
+    stage.copy(lds[b][0], k + j * a.k_row, a.k_row, e.lk - (int)j, a.dim);
+    stage.copy(lds[b][1], v + j * a.v_row, a.v_row, e.lk - (int)j, a.dim);
   };
-  if (t1 > 0) {
-    load(0);
-    ks.store(lds[0][0]);
-    vs.store(lds[0][1]);
-  }
-  __syncthreads();
-  for (int t = 0; t < t1; ++t) {
-    const char* kt = lds[t & 1][0];
-    const char* vt = lds[t & 1][1];
-    if (t + 1 < t1) load(t + 1);
+  if (t0 < t1) load(t0, 0);
+  wait_copies();
+  for (int t = t0; t < t1; ++t) {
+    const char* kt = lds[(t - t0) & 1][0];
+    const char* vt = lds[(t - t0) & 1][1];
+    if (t + 1 < t1) load(t + 1, (t + 1 - t0) & 1);
     if (t * BN < seen_max) {
 #pragma unroll
       for (int n = 0; n < BN / 32; ++n) {
@@ -595,8 +686,8 @@ __global__ __launch_bounds__(NW * 64) void k_attention_dq(AttnArgs a) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const int key = t * BN + 32 * n + 8 * (i / 4) + 4 * h + i % 4;
-          const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], c, -lse2));
-          x[i] = p * (y[i] - delta);
+          const float pr = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], c, -lse2));
+          x[i] = pr * (y[i] - delta);
           if (mask && key >= seen) x[i] = 0.f;
         }
 #pragma unroll
@@ -607,33 +698,38 @@ __global__ __launch_bounds__(NW * 64) void k_attention_dq(AttnArgs a) {
         }
       }
     }
-    if (t + 1 < t1) {
-      ks.store(lds[(t + 1) & 1][0]);
-      vs.store(lds[(t + 1) & 1][1]);
-    }
-    __syncthreads();
+    wait_copies();
   }
   if (r < rows) {
 #pragma unroll
-    for (int d = 0; d < D / 32; ++d) store_col<T>((T*)a.dq + at * a.dim, g[d], 32 * d, a.dim, a.scale);
+    for (int d = 0; d < D / 32; ++d) {
+      if (a.n_split > 1)
+        store_col<float>(a.part + (blockIdx.y * a.n_q * a.heads + at) * a.dim, g[d], 32 * d, a.dim, a.scale);
+      else
+        store_col<T>((T*)a.dq + at * a.dim, g[d], 32 * d, a.dim, a.scale);
+    }
   }
 }
 
 // dK and dV: waves of 32 keys over the packed rows that see them.
 //   S = Q K^T, dP = dO V^T, dV^T += dO^T P, dK^T += Q^T dS.
 template <class T, int D, int NW, int BQ>
-__global__ __launch_bounds__(NW * 64) void k_attention_dkv(AttnArgs a) {
+__global__ __launch_bounds__(NW * 64, (Plan<T, D>::kDkvWaves)) void k_attention_dkv(AttnArgs a) {
   using L = Tile<T, D, BQ>;
   constexpr int NT = NW * 64, BK = NW * 32;
   __shared__ __attribute__((aligned(16))) char lds[2][2][L::kBytes];
   __shared__ float stat[2][2][BQ];
+  using LK = Tile<T, D, BK>;
+  constexpr bool kLds = Plan<T, D>::kValuesInLds;
+  __shared__ __attribute__((aligned(16))) char vt[kLds ? LK::kBytes : 16];
   const int kvh = (int)(blockIdx.x % (unsigned)a.kv_heads);
-  const int64_t slot = blockIdx.x / (unsigned)a.kv_heads;
-  int64_t first;
-  const int s = seq_of_slot(a.k_off, a.n_seq, a.n_k, 1, BK, slot, &first);
-  const Seq e = seq_of(a, s);
-  const int64_t j0_64 = (slot - first) * BK;
-  if (j0_64 < 0 || j0_64 >= e.lk) return;
+  const Place p = place_of(a.k_off, a.n_seq, a.n_k, 1, BK, blockIdx.x / (unsigned)a.kv_heads,
+                           gridDim.x / (unsigned)a.kv_heads);
+  if (p.s < 0) return;
+  const Seq e = seq_of(a, p.s);
+  // Early keys are seen by the most rows.
+  const int64_t j0_64 = (int64_t)(p.n ? p.n - 1 - p.at : p.at) * BK;
+  if (j0_64 >= e.lk) return;
   const int j0 = (int)j0_64;
   const int rows = e.lq * a.group;
   const int w = wave(), l32 = lane() & 31, h = lane() >> 5;
@@ -641,18 +737,23 @@ __global__ __launch_bounds__(NW * 64) void k_attention_dkv(AttnArgs a) {
   // First query that sees any key of the tile.
   int q_first = a.causal ? j0 - (e.lk - e.lq) : 0;
   q_first = q_first < 0 ? 0 : q_first > e.lq ? e.lq : q_first;
-  const int t0 = q_first * a.group / BQ, t1 = (rows + BQ - 1) / BQ;
+  int t0 = q_first * a.group / BQ, t1 = (rows + BQ - 1) / BQ;
+  if (a.n_split > 1) {
+    const int per = (t1 - t0 + a.n_split - 1) / a.n_split;
+    t0 += (int)blockIdx.y * per;
+    t1 = t0 + per < t1 ? t0 + per : t1;
+  }
 
   const T* q = (const T*)a.q + e.q0 * a.q_row + (int64_t)kvh * a.group * a.q_head;
   const int64_t at0 = e.q0 * a.heads + (int64_t)kvh * a.group;
   const T* k = (const T*)a.k + e.k0 * a.k_row + (int64_t)kvh * a.k_head;
   const T* v = (const T*)a.v + e.k0 * a.v_row + (int64_t)kvh * a.v_head;
-  frag_t<T> kf[D / 16], vf[D / 16];
+  frag_t<T> kf[D / 16], vf[kLds ? 1 : D / 16];
   const bool valid = key < e.lk;
 #pragma unroll
   for (int i = 0; i < D / 16; ++i) {
     kf[i] = global_frag<T>(k + (int64_t)(valid ? key : 0) * a.k_row, valid, 16 * i, a.dim);
-    vf[i] = global_frag<T>(v + (int64_t)(valid ? key : 0) * a.v_row, valid, 16 * i, a.dim);
+    if constexpr (!kLds) vf[i] = global_frag<T>(v + (int64_t)(valid ? key : 0) * a.v_row, valid, 16 * i, a.dim);
   }
   f32x16 gk[D / 32], gv[D / 32];
 #pragma unroll
@@ -660,13 +761,14 @@ __global__ __launch_bounds__(NW * 64) void k_attention_dkv(AttnArgs a) {
   const float c = a.scale * kLog2e;
   constexpr float kUp = (float)(1 << Frag<T>::kShift), kDown = 1.f / kUp;
 
-  Stage<T, D, BQ, NT> qs, ds;
+  const Stage<T, D, BQ, NT> stage;
   float ss = 0.f, sd = 0.f;
-  const auto load = [&](int t) {
-    qs.load(a.dim, [&](int r) { return t * BQ + r < rows ? q + row_offset(a, t * BQ + r, a.q_row, a.q_head) : nullptr; });
-    ds.load(a.dim, [&](int r) {
-      return t * BQ + r < rows ? (const T*)a.dout + (at0 + row_offset(a, t * BQ + r, a.heads, 1)) * a.dim : nullptr;
-    });
+  const T* dout = (const T*)a.dout + at0 * a.dim;
+  const auto load = [&](int t, int b) {
+    stage.copy_packed(
+        lds[b][0], lds[b][1], a, t * BQ, rows,
+        [&](int i, int g) { return q + ((uint64_t)(uint32_t)i * (uint32_t)a.q_row + (uint64_t)(uint32_t)g * (uint32_t)a.q_head); },
+        [&](int i, int g) { return dout + (uint64_t)(uint32_t)(i * a.heads + g) * (uint32_t)a.dim; });
     if (threadIdx.x < BQ) {
       const int r = t * BQ + (int)threadIdx.x;
       const int64_t at = at0 + row_offset(a, r < rows ? r : rows - 1, a.heads, 1);
@@ -675,40 +777,44 @@ __global__ __launch_bounds__(NW * 64) void k_attention_dkv(AttnArgs a) {
     }
   };
   const auto store = [&](int b) {
-    qs.store(lds[b][0]);
-    ds.store(lds[b][1]);
     if (threadIdx.x < BQ) {
       stat[b][0][threadIdx.x] = ss;
       stat[b][1][threadIdx.x] = sd;
     }
   };
+  if constexpr (kLds) Stage<T, D, BK, NT>().copy(vt, v + j0 * a.v_row, a.v_row, e.lk - j0, a.dim);
   if (t0 < t1) {
-    load(t0);
+    load(t0, 0);
     store(0);
   }
-  __syncthreads();
+  wait_copies();
   for (int t = t0; t < t1; ++t) {
     const int b = (t - t0) & 1;
     const char* qt = lds[b][0];
     const char* dt = lds[b][1];
-    if (t + 1 < t1) load(t + 1);
+    if (t + 1 < t1) load(t + 1, (t + 1 - t0) & 1);
 #pragma unroll
     for (int n = 0; n < BQ / 32; ++n) {
       f32x16 x = zero16(), y = zero16();
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) x = mma(L::rows(qt, 32 * n, 16 * i), kf[i], x);
 #pragma unroll
-      for (int i = 0; i < D / 16; ++i) y = mma(L::rows(dt, 32 * n, 16 * i), vf[i], y);
+      for (int i = 0; i < D / 16; ++i) {
+        frag_t<T> f;
+        if constexpr (kLds) f = LK::rows(vt, 32 * w, 16 * i);
+        else f = vf[i];
+        y = mma(L::rows(dt, 32 * n, 16 * i), f, y);
+      }
       const int rn = t * BQ + 32 * n;
       // The tile's first row sees the fewest keys.
       const bool mask = a.causal && seen_keys(a, e, rn) < j0 + w * 32 + 32;
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const int rr = 8 * (i / 4) + 4 * h + i % 4;
-        float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], c, -stat[b][0][32 * n + rr]));
-        float g = p * __builtin_fmaf(y[i], kDown, -stat[b][1][32 * n + rr]);
-        if (mask && key >= seen_keys(a, e, rn + rr)) p = g = 0.f;
-        x[i] = p;
+        float pr = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], c, -stat[b][0][32 * n + rr]));
+        float g = pr * __builtin_fmaf(y[i], kDown, -stat[b][1][32 * n + rr]);
+        if (mask && key >= seen_keys(a, e, rn + rr)) pr = g = 0.f;
+        x[i] = pr;
         y[i] = g;
       }
 #pragma unroll
@@ -721,16 +827,33 @@ __global__ __launch_bounds__(NW * 64) void k_attention_dkv(AttnArgs a) {
       }
     }
     if (t + 1 < t1) store((t + 1 - t0) & 1);
-    __syncthreads();
+    wait_copies();
   }
   if (valid) {
-    const int64_t at = ((e.k0 + key) * a.kv_heads + kvh) * a.dim;
+    const int64_t at = ((e.k0 + key) * a.kv_heads + kvh) * a.dim, n = a.n_k * a.kv_heads * a.dim;
 #pragma unroll
     for (int d = 0; d < D / 32; ++d) {
-      store_col<T>((T*)a.dk + at, gk[d], 32 * d, a.dim, a.scale);
-      store_col<T>((T*)a.dv + at, gv[d], 32 * d, a.dim, kDown);
+      if (a.n_split > 1) {
+        store_col<float>(a.part + (2 * blockIdx.y) * n + at, gk[d], 32 * d, a.dim, a.scale);
+        store_col<float>(a.part + (2 * blockIdx.y + 1) * n + at, gv[d], 32 * d, a.dim, kDown);
+      } else {
+        store_col<T>((T*)a.dk + at, gk[d], 32 * d, a.dim, a.scale);
+        store_col<T>((T*)a.dv + at, gv[d], 32 * d, a.dim, kDown);
+      }
     }
   }
+}
+
+// out = the sum of `parts` arrays of n, `stride` apart, in order; four
+// elements a thread.
+template <class T>
+__global__ __launch_bounds__(256) void k_sum_parts(const float* part, int64_t n, int64_t stride, int parts, T* out) {
+  const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+  if (at >= n) return;
+  f32x4 x = *(const f32x4*)(part + at);
+  for (int s = 1; s < parts; ++s) x += *(const f32x4*)(part + s * stride + at);
+  using V = __attribute__((ext_vector_type(4))) T;
+  *(V*)(out + at) = __builtin_convertvector(x, V);
 }
 
 // ---------------------------------------------------------------------------
@@ -763,25 +886,43 @@ void attention_set_group(AttnArgs* a) {
   a->div_mul = (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << l) - d)) / d + 1);
 }
 
-constexpr int kFwdWaves = 4, kFwdTile = kFwdWaves * 32, kFwdKeys = 64;
+// Workgroups hold four waves of 32 rows or keys.
+constexpr int kWaves = 4, kTile = 32 * kWaves;
 
-int attention_splits(int64_t n_q, int64_t n_k, int n_seq, int heads, int kv_heads) {
-  const int group = heads / kv_heads;
-  const int64_t wgs = slots_of(n_q * group, kFwdTile, n_seq) * kv_heads;
-  const int64_t steps = n_k / n_seq / (2 * kFwdKeys);  // parts of two steps at least
-  int64_t n = 512 / wgs;
-  if (n > steps) n = steps;
+// Parts in which each tile's steps are taken so that there are `wanted`
+// workgroups, each with two steps at least on average.
+static int parts_of(int64_t workgroups, int64_t wanted, int64_t steps) {
+  int64_t n = (wanted + workgroups - 1) / workgroups;
+  if (n > steps / 2) n = steps / 2;
   if (n > 64) n = 64;
   return n < 1 ? 1 : (int)n;
 }
 
+// The device holds two workgroups per CU.
+int attention_splits(int64_t n_q, int64_t n_k, int n_seq, int heads, int kv_heads) {
+  const int64_t workgroups = slots_of(n_q * (heads / kv_heads), kTile, n_seq) * kv_heads;
+  return workgroups > 256 ? 1 : parts_of(workgroups, 512, n_k / n_seq / 64);
+}
+
+AttnParts attention_back_parts(int64_t n_q, int64_t n_k, int n_seq, int heads, int kv_heads, int dim) {
+  AttnParts p;
+  const int64_t rows = n_q * (heads / kv_heads);
+  const int64_t wq = slots_of(rows, kTile, n_seq) * kv_heads, wk = slots_of(n_k, kTile, n_seq) * kv_heads;
+  p.dq = wq > 256 ? 1 : parts_of(wq, 512, n_k / n_seq / 64);
+  p.dkv = parts_of(wk, 1024, rows / n_seq / 64);
+  const int64_t a = p.dq > 1 ? p.dq * n_q * heads : 0, b = p.dkv > 1 ? 2 * p.dkv * n_k * kv_heads : 0;
+  p.bytes = (size_t)(a > b ? a : b) * dim * sizeof(float);
+  return p;
+}
+
 hipError_t launch_attention(const AttnArgs& a, int dtype, hipStream_t s) {
-  const int64_t wgs = slots_of(a.n_q * a.group, kFwdTile, a.n_seq) * a.kv_heads;
+  const int64_t workgroups = slots_of(a.n_q * a.group, kTile, a.n_seq) * a.kv_heads;
   return by_type(dtype, [&](auto t) {
     using T = decltype(t);
-    hipError_t err = by_dim(a.dim, [&](auto d) {
-      k_attention<T, decltype(d)::value, 1, kFwdWaves, kFwdKeys>
-          <<<dim3((unsigned)wgs, (unsigned)a.n_split), kFwdWaves * 64, 0, s>>>(a);
+    const hipError_t err = by_dim(a.dim, [&](auto d) {
+      constexpr int D = decltype(d)::value;
+      k_attention<T, D, 1, kWaves, Plan<T, D>::kKeys>
+          <<<dim3((unsigned)workgroups, (unsigned)a.n_split), kWaves * 64, 0, s>>>(a);
       return hipGetLastError();
     });
     if (err != hipSuccess || a.n_split == 1) return err;
@@ -790,26 +931,46 @@ hipError_t launch_attention(const AttnArgs& a, int dtype, hipStream_t s) {
   });
 }
 
-hipError_t launch_attention_backward(const AttnArgs& a, int dtype, hipStream_t s) {
+template <class T>
+static hipError_t sum_parts(const float* part, int64_t n, int64_t stride, int parts, void* out, hipStream_t s) {
+  k_sum_parts<T><<<(unsigned)((n / 4 + 255) / 256), 256, 0, s>>>(part, n, stride, parts, (T*)out);
+  return hipGetLastError();
+}
+
+hipError_t launch_attention_backward(AttnArgs a, int dtype, hipStream_t s) {
+  const AttnParts parts = attention_back_parts(a.n_q, a.n_k, a.n_seq, a.heads, a.kv_heads, a.dim);
   return by_type(dtype, [&](auto t) {
     using T = decltype(t);
+    hipError_t err = hipSuccess;
     if (a.n_q > 0) {
       k_attention_delta<T><<<(unsigned)((a.n_q * a.heads + 15) / 16), 256, 0, s>>>(a);
-      hipError_t err = hipGetLastError();
+      if ((err = hipGetLastError()) != hipSuccess) return err;
+      a.n_split = parts.dq;
+      err = by_dim(a.dim, [&](auto d) {
+        constexpr int D = decltype(d)::value;
+        const int64_t workgroups = slots_of(a.n_q * a.group, kTile, a.n_seq) * a.kv_heads;
+        k_attention_dq<T, D, kWaves, Plan<T, D>::kDqKeys>
+            <<<dim3((unsigned)workgroups, (unsigned)a.n_split), kWaves * 64, 0, s>>>(a);
+        return hipGetLastError();
+      });
+      const int64_t n = a.n_q * a.heads * a.dim;
+      if (err == hipSuccess && parts.dq > 1) err = sum_parts<T>(a.part, n, n, parts.dq, a.dq, s);
       if (err != hipSuccess) return err;
     }
-    return by_dim(a.dim, [&](auto d) {
-      constexpr int D = decltype(d)::value;
-      constexpr int B = sizeof(T) == 4 ? 32 : 64;
-      if (a.n_q > 0)
-        k_attention_dq<T, D, 4, B>
-            <<<(unsigned)(slots_of(a.n_q * a.group, 128, a.n_seq) * a.kv_heads), 256, 0, s>>>(a);
-      hipError_t err = hipGetLastError();
-      if (err != hipSuccess) return err;
-      if (a.n_k > 0)
-        k_attention_dkv<T, D, 4, B><<<(unsigned)(slots_of(a.n_k, 128, a.n_seq) * a.kv_heads), 256, 0, s>>>(a);
-      return hipGetLastError();
-    });
+    if (a.n_k > 0) {
+      a.n_split = parts.dkv;
+      err = by_dim(a.dim, [&](auto d) {
+        constexpr int D = decltype(d)::value;
+        const int64_t workgroups = slots_of(a.n_k, kTile, a.n_seq) * a.kv_heads;
+        k_attention_dkv<T, D, kWaves, Plan<T, D>::kDkvRows>
+            <<<dim3((unsigned)workgroups, (unsigned)a.n_split), kWaves * 64, 0, s>>>(a);
+        return hipGetLastError();
+      });
+      const int64_t n = a.n_k * a.kv_heads * a.dim;
+      if (err == hipSuccess && parts.dkv > 1) err = sum_parts<T>(a.part, n, 2 * n, parts.dkv, a.dk, s);
+      if (err == hipSuccess && parts.dkv > 1) err = sum_parts<T>(a.part + n, n, 2 * n, parts.dkv, a.dv, s);
+    }
+    return err;
   });
 }
 
