@@ -18,13 +18,19 @@ namespace {
 
 using namespace ocr;
 
-// Calls f(tensor, first element, elements) for the workgroup's chunks.
-template <class F>
+// Calls f(tensor, first element, elements) for the workgroup's chunks, in
+// ascending order or from the end backwards.
+template <bool BACK, class F>
 __device__ __forceinline__ void each_chunk(const ClipBatch& b, F f) {
-  int t = 0;
   const uint32_t n = b.first[b.n];
-  for (uint32_t c = blockIdx.x; c < n; c += gridDim.x) {
-    while (b.first[t + 1] <= c) ++t;
+  int t = BACK ? b.n - 1 : 0;
+  for (uint32_t k = blockIdx.x; k < n; k += gridDim.x) {
+    const uint32_t c = BACK ? n - 1 - k : k;
+    if constexpr (BACK) {
+      while (b.first[t] > c) --t;
+    } else {
+      while (b.first[t + 1] <= c) ++t;
+    }
     const int64_t at = (int64_t)(c - b.first[t]) * kClipChunk;
     const int64_t left = b.count[t] - at;
     f(t, at, (int)(left < kClipChunk ? left : kClipChunk));
@@ -57,7 +63,7 @@ __device__ __forceinline__ double block_sum(double s) {
 
 __global__ __launch_bounds__(256) void k_square_sums(ClipBatch b, double* parts) {
   double s = 0;
-  each_chunk(b, [&](int t, int64_t at, int n) {
+  each_chunk<false>(b, [&](int t, int64_t at, int n) {
     if (b.type[t] == kF32) s += square_sum((const float*)b.in[t] + at, n);
     else if (b.type[t] == kF16) s += square_sum((const _Float16*)b.in[t] + at, n);
     else s += square_sum((const __bf16*)b.in[t] + at, n);
@@ -81,7 +87,8 @@ __global__ __launch_bounds__(256) void k_clip(ClipBatch b, const double* parts, 
   if (blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)root;
   const double r = (double)max_norm / (root + 1e-6);
   const float f = r < 1.0 ? (float)r : r != r ? __builtin_nanf("") : 1.f;
-  each_chunk(b, [&](int t, int64_t at, int n) {
+  // What the sums read last is what the caches still hold.
+  each_chunk<true>(b, [&](int t, int64_t at, int n) {
     // A factor of one leaves what is clipped in place as it is.
     if (f == 1.f && b.in[t] == b.out[t]) return;
     if (b.type[t] == kF32) scale_to((const float*)b.in[t] + at, (float*)b.out[t] + at, n, f);

@@ -25,6 +25,7 @@ namespace {
 using namespace ocr;
 
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
 #define OC_INF __builtin_inff()
 constexpr int kNone = 0x7fffffff;   // index of no element
 constexpr int kCap = 1024;          // entries of a wave's list
@@ -33,26 +34,28 @@ constexpr int kStep = 512;          // elements that a wave takes at a time
 __device__ __forceinline__ int lane() { return (int)(threadIdx.x & 63); }
 __device__ __forceinline__ int wave() { return __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)); }
 
-// exp(z), and z bounded for the product exp(z) z, which is 0 at -infinity.
-__device__ __forceinline__ float expn(float z) { return __builtin_amdgcn_exp2f(z * kLog2e); }
+// 2^z, and z bounded for the product 2^z z, which is 0 at -infinity.
+__device__ __forceinline__ float exp2n(float z) { return __builtin_amdgcn_exp2f(z); }
 __device__ __forceinline__ float bounded(float z) { return fmaxf(z, -1e4f); }
 
-// Running maximum, sum of exponentials and of exponentials times exponents.
+// Running maximum m, and with z = log2(e) (x - m): sums of 2^z and of z 2^z.
+// base is log2(e) m as rounded: what it is off the product is common to all
+// terms and to the result's first term.
 struct Stat {
-  float m = -OC_INF, s = 0.f, t = 0.f;
+  float m = -OC_INF, base = 0.f, s = 0.f, t = 0.f;
 
   __device__ __forceinline__ void rescale(float now) {
-    if (now == m || m == -OC_INF) {
-      m = now;
-      return;
+    const float next = now == -OC_INF ? 0.f : now * kLog2e;
+    if (now != m && m != -OC_INF) {
+      const float d = base - next, f = exp2n(d);
+      t = f * (t + s * bounded(d));
+      s *= f;
     }
-    const float d = m - now, f = expn(d);
-    t = f * (t + s * bounded(d));
-    s *= f;
     m = now;
+    base = next;
   }
   __device__ __forceinline__ void add(float x) {
-    const float z = x - m, e = expn(z);
+    const float z = __builtin_fmaf(x, kLog2e, -base), e = exp2n(z);
     s += e;
     t += e * bounded(z);
   }
@@ -63,21 +66,30 @@ struct Stat {
     s += o.s;
     t += o.t;
   }
+  __device__ __forceinline__ bool empty() const { return m == -OC_INF && s == 0.f; }  // every class ruled out
+  __device__ __forceinline__ float lse() const { return empty() ? -OC_INF : (base + log2f(s)) * kLn2; }
+  __device__ __forceinline__ float entropy() const {
+    const float h = (log2f(s) - t / s) * kLn2;
+    return empty() || h < 0.f ? 0.f : h;
+  }
+  __device__ __forceinline__ void set(float m_, float s_, float t_) {
+    rescale(m_);
+    s = s_;
+    t = t_;
+  }
 };
 
 __device__ __forceinline__ Stat group_stat(Stat a, int width) {
   for (int i = width >> 1; i; i >>= 1) {
     Stat o;
-    o.m = __shfl_xor(a.m, i);
-    o.s = __shfl_xor(a.s, i);
-    o.t = __shfl_xor(a.t, i);
+    o.set(__shfl_xor(a.m, i), __shfl_xor(a.s, i), __shfl_xor(a.t, i));
     a.join(o);
   }
   return a;
 }
 
 // Better first: greater value, then lower index.
-__device__ __forceinline__ bool better(float v, int i, float w, int j) { return v > w || (v == w && i < j); }
+__device__ __forceinline__ bool better(float v, int i, float w, int j) { return (v > w) | ((v == w) & (i < j)); }
 
 __device__ __forceinline__ void group_best(float& v, int& i, int width) {
   for (int k = width >> 1; k; k >>= 1) {
@@ -93,16 +105,10 @@ __device__ __forceinline__ void group_best(float& v, int& i, int width) {
 // What a row's statistics say of its label.
 __device__ __forceinline__ void write_row(const LabelArgs& a, int64_t row, const Stat& st, float lse, float mine) {
   a.lse[row] = lse;
-  const bool none = st.m == -OC_INF && st.s == 0.f;  // every class ruled out
   const int label = a.labels[row];
-  a.logprob[row] = label < 0 || label >= a.classes ? 0.f : none ? -OC_INF : mine - lse;
-  if (a.entropy) {
-    const float h = logf(st.s) - st.t / st.s;
-    a.entropy[row] = none || h < 0.f ? 0.f : h;
-  }
+  a.logprob[row] = label < 0 || label >= a.classes ? 0.f : st.empty() ? -OC_INF : mine - lse;
+  if (a.entropy) a.entropy[row] = st.entropy();
 }
-
-__device__ __forceinline__ float lse_of(const Stat& st) { return st.m == -OC_INF && st.s == 0.f ? -OC_INF : st.m + logf(st.s); }
 
 template <class T>
 __device__ __forceinline__ float label_logit(const LabelArgs& a, int64_t row) {
@@ -172,22 +178,14 @@ __global__ __launch_bounds__(256) void k_labels_held(LabelArgs a) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) m = fmaxf(m, r.x[v][i]);
     m = group_max(m, a.lanes);
-    st.m = m;
-    if (m != -OC_INF) {
+    st.rescale(m);
 #pragma unroll
-      for (int v = 0; v < NV; ++v)
+    for (int v = 0; v < NV; ++v)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) st.add(r.x[v][i]);
-    } else {
-      // Nothing but -infinity, or NaN, which must show.
-#pragma unroll
-      for (int v = 0; v < NV; ++v)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) st.s += r.x[v][i] != r.x[v][i] ? r.x[v][i] : 0.f;
-    }
+      for (int i = 0; i < 8; ++i) st.add(r.x[v][i]);
     st.s = group_sum(st.s, a.lanes);
     st.t = group_sum(st.t, a.lanes);
-    const float lse = lse_of(st);
+    const float lse = st.lse();
     if (r.t == 0) write_row(a, row, st, lse, label_logit<T>(a, row));
     // The best of what comes after the last one found.
     float last = OC_INF;
@@ -220,7 +218,7 @@ struct Grad {
   bool none;
   __device__ __forceinline__ float operator()(float x) const {
     const float z = x - lse;
-    return none ? 0.f : -expn(z) * (g + ge * (bounded(z) + h));
+    return none ? 0.f : -exp2n(z * kLog2e) * (g + ge * (bounded(z) + h));
   }
 };
 
@@ -279,46 +277,107 @@ struct List {
     count += __popcll(all);
   }
 
-  // The list's `top` best, in order, at its front.  n <= kCap entries.
+  // Bounds the first elements: of every lane's greatest, x, the `top`-th is no
+  // better than the `top`-th of all.
+  __device__ __forceinline__ void start(float x, int top) {
+    const float k = kth(x, top);
+    const int b = (int)__float_as_uint(k);
+    // The next lower number, so that equal ones enter.
+    least = k == -OC_INF ? k : __uint_as_float(k > 0.f ? b - 1 : k < 0.f ? b + 1 : 0x80000001);
+    next = 64 + top;
+  }
+
+  // Keeps the list's `top` best (at most 32), in order, at its front.
+  //
+  // Entries e stand in lane e % 64.  While there are more than 64 of them, the
+  // `top`-th of the lanes' best bounds the list's `top` best from below, and
+  // what is worse goes: first by value alone, which is quick and leaves few
+  // unless many are equal; then by value and index, which leaves entries in
+  // `top` lanes only, at most half.  Of 64 entries, one per lane, each lane
+  // counts those that are better than its own, which is its place.
   __device__ __forceinline__ void shrink(int top) {
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    float x[kCap / 64];
-    int j[kCap / 64];
+    sync();
+    bool equal = false;
+    while (count > 64) {
+      const int had = count;
+      float x[kCap / 64], best = -OC_INF;
+      int j[kCap / 64], best_j = kNone;
 #pragma unroll
-    for (int k = 0; k < kCap / 64; ++k) {
-      const int at = lane() + 64 * k;
-      x[k] = at < count ? v[at] : -OC_INF;
-      j[k] = at < count ? i[at] : kNone;
-    }
-    __builtin_amdgcn_wave_barrier();
-    float last = OC_INF;
-    int last_i = -1, found = 0;
-    for (int k = 0; k < top; ++k) {
-      float best = -OC_INF;
-      int best_i = kNone;
-#pragma unroll
-      for (int e = 0; e < kCap / 64; ++e)
-        if (j[e] != kNone && better(last, last_i, x[e], j[e]) && better(x[e], j[e], best, best_i)) {
-          best = x[e];
-          best_i = j[e];
+      for (int k = 0; k < kCap / 64; ++k) {
+        x[k] = -OC_INF;
+        j[k] = kNone;
+        if (64 * k < had) {
+          const int at = lane() + 64 * k;
+          if (at < had) {
+            x[k] = v[at];
+            j[k] = i[at];
+          }
+          const bool up = better(x[k], j[k], best, best_j);
+          best = up ? x[k] : best;
+          best_j = up ? j[k] : best_j;
         }
-      group_best(best, best_i, 64);
-      best_i = __builtin_amdgcn_readfirstlane(best_i);
-      if (best_i == kNone) break;
-      if (lane() == 0) {
-        v[k] = best;
-        i[k] = best_i;
       }
-      last = best;
-      last_i = best_i;
-      found = k + 1;
+      float bound;
+      int bound_j = kNone;
+      if (!equal) {
+        bound = kth(best, top);
+      } else {
+        const int l = __ffsll((unsigned long long)__ballot(place(best, best_j, 64) == top - 1)) - 1;
+        bound = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(best), l));
+        bound_j = __builtin_amdgcn_readlane(best_j, l);
+      }
+      sync();
+      count = 0;
+#pragma unroll
+      for (int k = 0; k < kCap / 64; ++k)
+        if (64 * k < had) push((j[k] != kNone) & !better(bound, bound_j, x[k], j[k]), x[k], j[k]);
+      sync();
+      equal = 2 * count > had;
     }
+    const float x = lane() < count ? v[lane()] : -OC_INF;
+    const int j = lane() < count ? i[lane()] : kNone;
+    const int at = place(x, j, count);
+    sync();
+    if (lane() < count && at < top) {
+      v[at] = x;
+      i[at] = j;
+    }
+    if (count >= top) {
+      const int l = __ffsll((unsigned long long)__ballot((lane() < count) & (at == top - 1))) - 1;
+      least = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), l));
+      count = top;
+    }
+    sync();
+    next = 64 + top;
+  }
+
+  // The k-th greatest of the lanes' x, bit by bit; NaN counts as -infinity.
+  static __device__ __forceinline__ float kth(float x, int k) {
+    const uint32_t b = __float_as_uint(x == x ? x + 0.f : -OC_INF), key = b ^ ((uint32_t)((int)b >> 31) | 0x80000000u);  // same order
+    uint32_t r = 0;
+    for (int i = 31; i >= 0; --i) {
+      const uint32_t up = r | (1u << i);
+      if (__popcll(__ballot(key >= up)) >= k) r = up;
+    }
+    return __uint_as_float(r ^ ((uint32_t)((int)~r >> 31) | 0x80000000u));
+  }
+
+  // How many of the first n lanes hold something better than this one.
+  static __device__ __forceinline__ int place(float x, int j, int n) {
+    int r = 0;
+    for (int l = 0; l < n; l += 8)  // lanes past the n-th hold nothing better
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float y = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), l + k));
+        r += better(y, __builtin_amdgcn_readlane(j, l + k), x, j) ? 1 : 0;
+      }
+    return r;
+  }
+
+  // Orders this wave's accesses to its list.
+  static __device__ __forceinline__ void sync() {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
-    count = found;
-    least = found == top ? last : -OC_INF;
-    next = kCap - kStep;
   }
 };
 
@@ -357,37 +416,52 @@ __global__ __launch_bounds__(256) void k_labels_streamed(LabelArgs a) {
   const int j0 = (int)blockIdx.y * a.per, j1 = j0 + a.per < a.classes ? j0 + a.per : a.classes;
   const T* x = (const T*)a.logits + row * a.classes + j0;
   const int n = j1 - j0, head = head_of(x, n), body = (n - head) / 8, w = wave();
-  List list{vals + (TOP ? w * kCap : 0), idxs + (TOP ? w * kCap : 0), 0, 1, -OC_INF};
+  List list{vals + (TOP ? w * kCap : 0), idxs + (TOP ? w * kCap : 0), 0, 0, -OC_INF};
   Stat st;
 
   const auto one = [&](bool in, int j) {
     const float y = in ? (float)x[j] : -OC_INF;
     if (y > st.m) st.rescale(y);
-    if (in && (st.m != -OC_INF || y != y)) st.add(y);
+    if (in) st.add(y);
     if (TOP) list.push(in && y > list.least, y, j0 + j);
   };
   if (w == 0 && head) one(lane() < head, lane());
-  for (int v = (int)threadIdx.x; v - lane() < body; v += 256) {
-    f32x8 y;
+  // Two vectors per lane are on their way while one is worked on.  The loop
+  // is not unrolled: its list handling would not fit the instruction cache.
+  using Raw = typename Vec8<T>::type;
+  const T* from = x + head;
+  const auto fetch = [&](int v0, Raw& r) {
+    const int v = v0 + lane();
+    if (v < body) r = *(const Raw*)(from + 8 * (int64_t)v);
+  };
+  Raw r0 = {}, r1 = {}, r2 = {};
+  fetch(64 * w, r0);
+  fetch(64 * w + 256, r1);
+#pragma unroll 1
+  for (int v0 = 64 * w; v0 < body; v0 += 256) {
+    fetch(v0 + 512, r2);
+    const int v = v0 + lane();
+    f32x8 y = __builtin_convertvector(r0, f32x8);
+    r0 = r1;
+    r1 = r2;
+    if (v >= body) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = -OC_INF;
-    if (v < body) y = load8(x + head + 8 * (int64_t)v);
+      for (int i = 0; i < 8; ++i) y[i] = -OC_INF;
+    }
     float top = y[0];
 #pragma unroll
     for (int i = 1; i < 8; ++i) top = fmaxf(top, y[i]);
     if (top > st.m) st.rescale(top);
-    // A maximum of -infinity so far: only NaN counts.
-    const float base = st.m == -OC_INF ? 0.f : st.m;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float z = y[i] - base, e = expn(z);
-      st.s += e;
-      st.t += e * bounded(z);
-    }
+    for (int i = 0; i < 8; ++i) st.add(y[i]);
     if constexpr (TOP) {
+      if (list.next == 0) list.start(top, a.top);
       if (__ballot(top > list.least)) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) list.push(y[i] > list.least, y[i], j0 + head + 8 * v + i);
+        for (int i = 0; i < 8; ++i) {
+          const bool take = y[i] > list.least;
+          if (__ballot(take)) list.push(take, y[i], j0 + head + 8 * v + i);
+        }
         if (list.count >= list.next) list.shrink(a.top);
       }
     }
@@ -409,9 +483,7 @@ __global__ __launch_bounds__(256) void k_labels_streamed(LabelArgs a) {
   if (w) return;
   for (int i = 1; i < 4; ++i) {
     Stat o;
-    o.m = stats[0][i];
-    o.s = stats[1][i];
-    o.t = stats[2][i];
+    o.set(stats[0][i], stats[1][i], stats[2][i]);
     st.join(o);
   }
   if constexpr (TOP) {
@@ -435,7 +507,7 @@ __global__ __launch_bounds__(256) void k_labels_streamed(LabelArgs a) {
     }
     return;
   }
-  const float lse = lse_of(st);
+  const float lse = st.lse();
   if (lane() == 0) write_row(a, row, st, lse, label_logit<T>(a, row));
   if constexpr (TOP) finish_top<T>(a, row, list.v, list.i, list.count, lse);
 }
@@ -450,16 +522,14 @@ __global__ __launch_bounds__(64) void k_labels_join(LabelArgs a) {
   for (int p = lane(); p < a.parts; p += 64) {
     Stat o;
     const float* q = a.part_stat + 3 * (row * a.parts + p);
-    o.m = q[0];
-    o.s = q[1];
-    o.t = q[2];
+    o.set(q[0], q[1], q[2]);
     st.join(o);
   }
   st = group_stat(st, 64);
-  const float lse = lse_of(st);
+  const float lse = st.lse();
   if (lane() == 0) write_row(a, row, st, lse, label_logit<T>(a, row));
   if constexpr (TOP) {
-    List list{vals, idxs, 0, 1, -OC_INF};
+    List list{vals, idxs, 0, 0, -OC_INF};
     const int n = a.parts * a.top;
     for (int e = 0; e < n; e += 64) {
       if (list.count > kCap - 64) list.shrink(a.top);

@@ -143,12 +143,17 @@ __global__ __launch_bounds__(WIDE ? 1024 : 256) void k_rms_norm_back(NormArgs a)
     const int64_t row = first + mine;
     const bool live = row < a.rows;
     const int64_t at = (live ? row : a.rows - 1) * a.c;
-    f32x8 h[NV], d[NV];
+    f32x8 h[NV], d[NV], e[NV];
     float sq = 0.f, dot = 0.f;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       h[v] = col.load((const TS*)a.sum + at, v);
       d[v] = col.load((const TY*)a.dy + at, v);
+      e[v] = f32x8{0, 0, 0, 0, 0, 0, 0, 0};
+    }
+    if (a.dsum) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v) e[v] = col.load((const TS*)a.dsum + at, v);
     }
 #pragma unroll
     for (int v = 0; v < NV; ++v)
@@ -165,9 +170,7 @@ __global__ __launch_bounds__(WIDE ? 1024 : 256) void k_rms_norm_back(NormArgs a)
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
         dw[v] += d[v] * (h[v] * r);
-        f32x8 g = (d[v] * w[v] - h[v] * k) * r;
-        if (a.dsum) g += col.load((const TS*)a.dsum + at, v);
-        col.store((TS*)a.dx + at, v, g);
+        col.store((TS*)a.dx + at, v, (d[v] * w[v] - h[v] * k) * r + e[v]);
       }
     }
   }
@@ -216,7 +219,7 @@ struct Shape {
 
 Shape shape_of(int c) {
   Shape s{1, 1, 256, false};
-  s.nv = c <= 512 ? 1 : 4;
+  s.nv = c <= 512 ? 1 : c <= 1024 ? 2 : 4;
   const int n = (c + 8 * s.nv - 1) / (8 * s.nv);
   while (s.lanes < n) s.lanes <<= 1;
   if (s.lanes > 64) {
@@ -231,6 +234,7 @@ hipError_t by_shape(const Shape& s, bool vec, F f) {
   const auto go = [&](auto v) {
     if (s.wide) return f(v, std::integral_constant<int, 4>(), std::true_type());
     if (s.nv == 4) return f(v, std::integral_constant<int, 4>(), std::false_type());
+    if (s.nv == 2) return f(v, std::integral_constant<int, 2>(), std::false_type());
     return f(v, std::integral_constant<int, 1>(), std::false_type());
   };
   return vec ? go(std::true_type()) : go(std::false_type());

@@ -7,7 +7,7 @@
 namespace ocr {
 
 using f32x4 = __attribute__((ext_vector_type(4))) float;
-using f32x8 = __attribute__((ext_vector_type(8))) float;
+using f32x8 = __attribute__((ext_vector_type(8), aligned(16))) float;
 using bf16x8 = __attribute__((ext_vector_type(8))) __bf16;
 using f16x8 = __attribute__((ext_vector_type(8))) _Float16;
 using u32x2 = __attribute__((ext_vector_type(2))) uint32_t;
@@ -20,6 +20,10 @@ struct e4m3 {
 
 template <class T>
 struct Vec8;
+template <>
+struct Vec8<float> {
+  using type = f32x8;
+};
 template <>
 struct Vec8<__bf16> {
   using type = bf16x8;

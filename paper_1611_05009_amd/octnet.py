@@ -765,15 +765,25 @@ def clip_grad_norm(grads, max_norm: float, out=None, ws: torch.Tensor | None = N
     returns their common norm, a float32 scalar on the GPU (nothing waits for
     it)."""
     grads = list(grads)
-    out = grads if out is None else list(out)
-    if len(out) != len(grads) or any(a.shape != b.shape or a.dtype != b.dtype for a, b in zip(grads, out)):
-        raise OctNetError("out must match the gradients")
     n = len(grads)
-    norm = torch.empty((), dtype=torch.float32, device=grads[0].device if n else _dev())
-    src = (_P * n)(*[_ptr(t) for t in grads])
-    dst = src if out is grads else (_P * n)(*[_ptr(t) for t in out])
+    for t in grads:
+        if not (t.is_cuda and t.is_contiguous()):
+            raise OctNetError("expected contiguous GPU tensors")
+        if t.dtype not in _TYPES:
+            raise OctNetError("expected float32, float16 or bfloat16, got %s" % t.dtype)
+    src = (_P * n)(*[t.data_ptr() for t in grads])
+    dst = src
+    if out is not None:
+        out = list(out)
+        if len(out) != n:
+            raise OctNetError("out must match the gradients")
+        for t, o in zip(grads, out):
+            if o.dtype != t.dtype or o.shape != t.shape or not (o.is_cuda and o.is_contiguous()):
+                raise OctNetError("out must match the gradients")
+        dst = (_P * n)(*[o.data_ptr() for o in out])
     counts = (_L * n)(*[t.numel() for t in grads])
-    types = (_I * n)(*[_type(t) for t in grads])
+    types = (_I * n)(*[_TYPES[t.dtype] for t in grads])
+    norm = torch.empty((), dtype=torch.float32, device=grads[0].device if n else _dev())
     if ws is None:
         nb = ctypes.c_size_t(0)
         _check(lib().oc_clip_grad_norm_workspace(counts, n, ctypes.byref(nb)), "oc_clip_grad_norm_workspace")

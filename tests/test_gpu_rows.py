@@ -277,6 +277,19 @@ def test_labels_few_left():
     assert b.entropy is None and float(b.logprob[1]) == 0.0 and float(b.logprob[2]) == 0.0
 
 
+def test_labels_after_nan():
+    """The first thousands of a long row are NaN, as are single places later:
+    the alternatives come from the rest."""
+    from paper_1611_05009_amd import octnet as oc
+    x = randn(6, 2, 30000)
+    x[0, :2500] = math.nan
+    x[0, 5000::7] = math.nan
+    a = oc.label_logprobs(x.cuda(), torch.tensor([1, 2], dtype=torch.int32).cuda(), top=8)
+    order = torch.sort(torch.where(torch.isnan(x[0]), torch.tensor(-math.inf), x[0]), descending=True, stable=True).indices[:8]
+    assert torch.equal(a.top_label[0].cpu().long(), order) and math.isnan(a.lse[0])
+    assert math.isfinite(a.lse[1])
+
+
 def test_labels_gradient_against_differences():
     """Central differences of the 64-bit loss along a direction; error of
     order t^2 = 1e-10, gradients in float."""
