@@ -103,56 +103,94 @@ __device__ __forceinline__ frag_t<T> to_frag(const f32x16& c, int first) {
 }
 
 // A tile of R rows of up to D elements in LDS: rows of P elements (P the
-// power of two from D up) in 16-byte chunks, chunk c of row r at position
-// c ^ swizzle(r).  Eight consecutive rows at one chunk (a row-wise fragment
-// read) and four rows at two neighbouring chunks (a transposing read) then
-// touch every bank once.
+// power of two from D up) in 16-byte chunks, laid out in groups of 1024 bytes,
+// what one wave copies at a time.  LDS serves 256 bytes a cycle from 64 banks:
+// 16 rows at one chunk (a row-wise fragment read), or four rows at four
+// neighbouring chunks (a transposing read).  Both are free of conflicts
+// because in the 256-byte lines of a group the chunks change places by the
+// line's number, and (where 16 rows are more than a group) each group starts
+// one chunk further.  Changing places by four bits of the row does the same,
+// but leaves twice as many addresses in registers, which the gradients do not
+// have.  (Before, LDS was busy half of the time at head size 128, and half of
+// that with conflicts.)  32-bit products take 16 times as long, and their
+// reads need no such care.
 template <class T, int D, int R>
 struct Tile {
   static constexpr int kPer = 16 / (int)sizeof(T);        // elements per chunk
   static constexpr int P = D <= 32 ? 32 : D <= 64 ? 64 : 128;
   static constexpr int kChunks = P / kPer;                // chunks per row: 4, 8, 16 or 32
-  static constexpr int kBytes = R * P * (int)sizeof(T);
+  static constexpr int kGroup = 64 / kChunks;             // rows of a group
+  static constexpr int kPad = sizeof(T) == 2 && kChunks >= 8 ? 16 : 0;
+  static constexpr int kBytes = R / kGroup * (1024 + kPad);
+  static_assert(R % 16 == 0, "whole fragments");
 
   static __device__ __forceinline__ int swizzle(int r) {
-    return kChunks >= 8 ? (((r & 3) << 1) | ((r >> 2) & 1)) : ((r & 2) | ((r >> 2) & 1));
+    if constexpr (sizeof(T) == 4) return ((r & 3) << 1) | ((r >> 2) & 1);
+    if constexpr (kChunks == 4) return (r >> 2) & 3;
+    if constexpr (kChunks == 8) return ((r << 1) & 4) | ((r >> 1) & 2);
+    return (r & 3) << 2;
   }
   static __device__ __forceinline__ int at(int r, int chunk) {
-    return (r * kChunks + (chunk ^ swizzle(r))) * 16;
+    return r * (kChunks * 16) + r / kGroup * kPad + (chunk ^ swizzle(r)) * 16;
+  }
+  // The same for `row` + r, row a multiple of 16.
+  static __device__ __forceinline__ int at(int row, int r, int chunk) {
+    return row * (kChunks * 16) + row / kGroup * kPad + at(r, chunk);
   }
 
+  // This lane's part of its addresses: those of a row-wise read start at
+  // row_at + row_x, those of a column read at col_at + col_x, and the column
+  // changes what the swizzle may change (kSwaps) by exclusive or.
+  static constexpr int kSwaps = kChunks == 4 ? 0x30 : kChunks == 8 ? 0x60 : 0xC0;
+  struct Lanes {
+    int row_at, row_x, col_at, col_x;
+    __device__ __forceinline__ Lanes() {
+      const int l = lane(), h = l >> 5;
+      int r = l & 31;
+      row_at = r * (kChunks * 16) + r / kGroup * kPad;
+      row_x = (h ^ swizzle(r)) * 16;
+      // Lanes of a group of 16 read four rows of 16 elements, four elements
+      // each, and get one column each.
+      r = 4 * h + ((l >> 2) & 3);
+      col_at = r * (kChunks * 16) + r / kGroup * kPad + (l & 1) * 8;
+      col_x = ((((l >> 3) & 2) | ((l >> 1) & 1)) ^ swizzle(r)) * 16;
+    }
+    // Keeps the addresses of a step from staying in registers over all steps.
+    __device__ __forceinline__ void renew() { asm volatile("" : "+v"(row_x), "+v"(col_x)); }
+  };
+  static constexpr int row_offset(int row) { return row * (kChunks * 16) + row / kGroup * kPad; }
+
   // Elements 8 h .. 8 h + 7 past `col` of row `row + lane % 32`.
-  static __device__ __forceinline__ frag_t<T> rows(const char* t, int row, int col) {
-    const int r = row + (lane() & 31), h = lane() >> 5;
+  static __device__ __forceinline__ frag_t<T> rows(const char* t, const Lanes& a, int row, int col) {
     if constexpr (sizeof(T) == 2) {
-      const u32x4 x = *(const u32x4*)(t + at(r, col / 8 + h));
+      const int c = col * 2;
+      const u32x4 x = *(const u32x4*)(t + a.row_at + (a.row_x ^ (c & kSwaps)) + (row_offset(row) + (c & ~kSwaps)));
       return __builtin_bit_cast(frag_t<T>, x);
     } else {
-      const f32x4 x = *(const f32x4*)(t + at(r, col / 4 + 2 * h));
-      const f32x4 y = *(const f32x4*)(t + at(r, col / 4 + 2 * h + 1));
+      const int r = lane() & 31, h = lane() >> 5;
+      const f32x4 x = *(const f32x4*)(t + at(row, r, col / 4 + 2 * h));
+      const f32x4 y = *(const f32x4*)(t + at(row, r, col / 4 + 2 * h + 1));
       return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
     }
   }
 
   // Rows row + 8 (i / 4) + 4 h + i % 4, i = 0..7, of column col + lane % 32.
-  static __device__ __forceinline__ frag_t<T> cols(const char* t, int row, int col) {
-    const int l = lane(), h = l >> 5;
+  static __device__ __forceinline__ frag_t<T> cols(const char* t, const Lanes& a, int row, int col) {
     if constexpr (sizeof(T) == 2) {
-      // Lanes of a group of 16 read four rows of 16 elements, four elements
-      // each, and get one column each.
-      const int r = row + 4 * h + ((l >> 2) & 3), c = col + (l & 16) + 4 * (l & 3);
       using lds4 = __attribute__((address_space(3))) i16x4;
-      const i16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(t + at(r, c / 8) + (c & 7) * 2));
-      const i16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(t + at(r + 8, c / 8) + (c & 7) * 2));
+      const int c = col * 2;
+      const char* p = t + a.col_at + (row_offset(row) + (c & ~kSwaps));
+      const char* q = p + (a.col_x ^ (c & kSwaps));
+      // Eight rows on, a line of four rows swaps by another number.
+      const char* q8 = kChunks == 4 ? p + (a.col_x ^ (c & kSwaps) ^ 0x20) : q;
+      const i16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)q);
+      const i16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(q8 + row_offset(8)));
       return __builtin_bit_cast(frag_t<T>, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
     } else {
-      const int c = col + (l & 31);
+      const int c = col + (lane() & 31), h = lane() >> 5;
       f32x8 x;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int r = row + 8 * (i / 4) + 4 * h + i % 4;
-        x[i] = *(const float*)(t + at(r, c / 4) + (c & 3) * 4);
-      }
+      for (int i = 0; i < 8; ++i) x[i] = *(const float*)(t + at(row, 8 * (i / 4) + 4 * h + i % 4, c / 4) + (c & 3) * 4);
       return x;
     }
   }
@@ -174,30 +212,39 @@ struct Stage {
   using L = Tile<T, D, R>;
   static constexpr int kN = R * L::kChunks / NT;    // chunks per thread
   static constexpr int kStep = NT / L::kChunks;     // rows between them
-  static_assert(R * L::kChunks % NT == 0 && kStep % 8 == 0, "whole waves, one swizzle per thread");
+  static_assert(R * L::kChunks % NT == 0, "whole waves");
 
-  int row, col;   // the thread's first row, and its column, in the tile
+  int row, chunk;  // the thread's first row, and its place in each of its rows
   __device__ __forceinline__ Stage() {
     row = (int)threadIdx.x / L::kChunks;
-    col = (((int)threadIdx.x % L::kChunks) ^ L::swizzle(row)) * L::kPer;
+    chunk = (int)threadIdx.x % L::kChunks;
+  }
+  // First element of the i-th chunk.
+  __device__ __forceinline__ int col(int i) const {
+    return (chunk ^ L::swizzle(kStep % 8 ? row + i * kStep : row)) * L::kPer;
   }
 
   static __device__ __forceinline__ void put(char* t, int i, const void* p) {
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p,
-                                     (__attribute__((address_space(3))) void*)(t + (wave() * 64 + i * NT) * 16), 16, 0, 0);
+    char* to = t + (wave() + i * (NT / 64)) * (1024 + L::kPad);
+    const uint32_t at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)to;
+    // As an instruction of its own: for the builtin the compiler waits for the
+    // whole copy before the next transposing read, of whatever buffer.  It
+    // writes no register, and wait_copies() waits for it.  (One wait state from
+    // the write of m0 to its use.)
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"{m0}"(at), "v"(p) : "memory");
   }
 
   // R rows from p on, `stride` elements apart, of which `rows` exist.
   __device__ __forceinline__ void copy(char* t, const T* p, int64_t stride, int rows, int dim) const {
-    const T* q = p + row * stride + col;
+    const T* q = p + row * stride;
     if (rows >= R && dim == D) {
 #pragma unroll
-      for (int i = 0; i < kN; ++i) put(t, i, q + i * kStep * stride);
+      for (int i = 0; i < kN; ++i) put(t, i, q + i * kStep * stride + col(i));
     } else {
 #pragma unroll
       for (int i = 0; i < kN; ++i) {
-        const bool in = (col < dim) & (row + i * kStep < rows);
-        put(t, i, in ? (const void*)(q + i * kStep * stride) : (const void*)&kZeros);
+        const bool in = (col(i) < dim) & (row + i * kStep < rows);
+        put(t, i, in ? (const void*)(q + i * kStep * stride + col(i)) : (const void*)&kZeros);
       }
     }
   }
@@ -209,10 +256,10 @@ struct Stage {
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
       const int n = r + row + i * kStep;
-      const bool in = (col < a.dim) & (n < rows);
+      const bool in = (col(i) < a.dim) & (n < rows);
       const int q = by_group(a, n), g = n - q * a.group;
-      put(tx, i, in ? (const void*)(at_x(q, g) + col) : (const void*)&kZeros);
-      put(ty, i, in ? (const void*)(at_y(q, g) + col) : (const void*)&kZeros);
+      put(tx, i, in ? (const void*)(at_x(q, g) + col(i)) : (const void*)&kZeros);
+      put(ty, i, in ? (const void*)(at_y(q, g) + col(i)) : (const void*)&kZeros);
     }
   }
 };
@@ -274,27 +321,27 @@ __device__ __forceinline__ Place place_of(const int64_t* off, int n_seq, int64_t
       const int64_t a = bounded(off[lane()], 0, rows), b = bounded(off[lane() + 1], a, rows);
       n = (int)(((b - a) * mul + tile - 1) / tile);
     }
-    int hi = n;  // one past the greatest number
-#pragma unroll
-    for (int i = 32; i; i >>= 1) {
-      const int o = __shfl_xor(hi, i);
+    // Least l of which at most x tiles have greater numbers: 64 candidates at
+    // a time, one per lane.
+    int hi = 0;  // one past the greatest number
+    for (int s = 0; s < n_seq; ++s) {
+      const int o = __builtin_amdgcn_readlane(n, s);
       hi = o > hi ? o : hi;
     }
-    hi = __builtin_amdgcn_readfirstlane(hi);
-    // Least l of which at most x tiles have greater numbers.
+    if (hi == 0) return p;
     int lo = 0, above = 0;
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      int more = n > mid + 1 ? n - mid - 1 : 0;
-#pragma unroll
-      for (int i = 32; i; i >>= 1) more += __shfl_xor(more, i);
-      more = __builtin_amdgcn_readfirstlane(more);
-      if (more <= x) {
-        hi = mid;
-        above = more;
-      } else {
-        lo = mid + 1;
+    for (int count = hi; count > 0;) {
+      const int step = (count + 63) / 64, l = lo + (lane() + 1) * step - 1;
+      int more = 0;
+      for (int s = 0; s < n_seq; ++s) {
+        const int o = __builtin_amdgcn_readlane(n, s) - l - 1;
+        more += o > 0 ? o : 0;
       }
+      // The last one qualifies: it is the greatest number, or the last found.
+      const int k = __ffsll((unsigned long long)__ballot(more <= x)) - 1;
+      above = __builtin_amdgcn_readlane(more, k);
+      lo += k * step;
+      count = step == 1 ? 0 : step;
     }
     uint64_t have = __ballot(n > lo);
     int skip = (int)(x - above);
@@ -326,6 +373,20 @@ __device__ __forceinline__ Place place_of(const int64_t* off, int n_seq, int64_t
   p.at = __builtin_amdgcn_readfirstlane((int)at);
   return p;
 }
+
+// A workgroup's head, part and tile.  Neighbouring numbers share a tile, so
+// that all parts of the tiles with the most work start first.
+struct Item {
+  int kvh, part;
+  int64_t tile, tiles;
+  __device__ __forceinline__ Item(const AttnArgs& a) {
+    const unsigned per = (unsigned)(a.kv_heads * a.n_split), x = blockIdx.x % per;
+    kvh = (int)(x % (unsigned)a.kv_heads);
+    part = (int)(x / (unsigned)a.kv_heads);
+    tile = blockIdx.x / per;
+    tiles = gridDim.x / per;
+  }
+};
 
 // Keys that packed row r of the sequence sees: the first `seen` ones.
 __device__ __forceinline__ int seen_keys(const AttnArgs& a, const Seq& e, int r) {
@@ -387,7 +448,7 @@ __device__ __forceinline__ void store_col(T* p, const f32x16& c, int d0, int dim
 template <class T, int D>
 struct Plan {
   static constexpr bool kWide = D > 64, kHalf = sizeof(T) == 2;
-  static constexpr int kKeys = kHalf || !kWide ? 64 : 32;       // forward
+  static constexpr int kKeys = kHalf && !kWide ? 128 : kHalf || !kWide ? 64 : 32;  // forward
   static constexpr int kDqKeys = kHalf ? 64 : 32;
   static constexpr int kDqWaves = kHalf || !kWide ? 2 : 1;
   static constexpr int kDkvRows = kHalf && !kWide ? 64 : 32;
@@ -406,9 +467,9 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention(AttnArgs a) {
   constexpr int NT = NW * 64, BM = NW * MT * 32;
   __shared__ __attribute__((aligned(16))) char lds[2][2][L::kBytes];
 
-  const int kvh = (int)(blockIdx.x % (unsigned)a.kv_heads);
-  const Place p = place_of(a.q_off, a.n_seq, a.n_q, a.group, BM, blockIdx.x / (unsigned)a.kv_heads,
-                           gridDim.x / (unsigned)a.kv_heads);
+  const Item item(a);
+  const int kvh = item.kvh;
+  const Place p = place_of(a.q_off, a.n_seq, a.n_q, a.group, BM, item.tile, item.tiles);
   if (p.s < 0) return;
   const Seq e = seq_of(a, p.s);
   const int rows = e.lq * a.group;
@@ -422,7 +483,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention(AttnArgs a) {
   int t0 = 0, t1 = (most + BN - 1) / BN;
   if (a.n_split > 1) {
     const int per = (t1 + a.n_split - 1) / a.n_split;
-    t0 = (int)blockIdx.y * per;
+    t0 = item.part * per;
     t1 = t0 + per < t1 ? t0 + per : t1;
   }
 
@@ -467,7 +528,9 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention(AttnArgs a) {
   };
   if (t0 < t1) load(t0, 0);
   wait_copies();
+  typename L::Lanes ln;
   for (int t = t0; t < t1; ++t) {
+    ln.renew();
     const char* kt = lds[(t - t0) & 1][0];
     const char* vt = lds[(t - t0) & 1][1];
     if (t + 1 < t1) load(t + 1, (t + 1 - t0) & 1);
@@ -479,10 +542,22 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention(AttnArgs a) {
         for (int m = 0; m < MT; ++m) x[m][n] = zero16();
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) {
-          const frag_t<T> kf = L::rows(kt, 32 * n, 16 * i);
+          const frag_t<T> kf = L::rows(kt, ln, 32 * n, 16 * i);
 #pragma unroll
           for (int m = 0; m < MT; ++m) x[m][n] = mma(kf, qf[m][i], x[m][n]);
         }
+      }
+      if constexpr (sizeof(T) == 2 && D > 64) {
+        // Four fragments ahead of the product that takes them (907 to 924
+        // TFLOP/s at head size 128; smaller ones have too few to gain).
+        constexpr int N = BN / 32 * (D / 16);
+        __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+        for (int i = 0; i < N - 4; ++i) {
+          __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x8, 4, 0);
       }
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
@@ -531,7 +606,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention(AttnArgs a) {
           for (int m = 0; m < MT; ++m) pf[m] = to_frag<T>(x[m][n], 8 * j);
 #pragma unroll
           for (int d = 0; d < D / 32; ++d) {
-            const frag_t<T> vf = L::cols(vt, 32 * n + 16 * j, 32 * d);
+            const frag_t<T> vf = L::cols(vt, ln, 32 * n + 16 * j, 32 * d);
 #pragma unroll
             for (int m = 0; m < MT; ++m) o[m][d] = mma(vf, pf[m], o[m][d]);
           }
@@ -550,7 +625,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention(AttnArgs a) {
     const int qi = by_group(a, r);
     const int64_t at = (e.q0 + qi) * a.heads + (int64_t)kvh * a.group + (r - qi * a.group);
     if (a.n_split > 1) {
-      const int64_t part = (int64_t)blockIdx.y * a.n_q * a.heads + at;
+      const int64_t part = (int64_t)item.part * a.n_q * a.heads + at;
       if (h == 0) a.part_lse[part] = lse;
 #pragma unroll
       for (int d = 0; d < D / 32; ++d) store_col<float>(a.part + part * a.dim, o[m][d], 32 * d, a.dim, f);
@@ -562,25 +637,33 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention(AttnArgs a) {
   }
 }
 
-// The parts of each row weighted by exp(lse_part - lse): one wave per row.
-template <class T>
+// The parts of each row weighted by exp(lse_part - lse), LANES lanes of four
+// elements per row.  All loads of a row are independent: one latency for the
+// statistics and one for the parts, however many there are.
+template <class T, int LANES>
 __global__ __launch_bounds__(256) void k_attention_join(AttnArgs a) {
-  const int64_t row = (int64_t)blockIdx.x * 4 + wave(), n = a.n_q * a.heads;
+  const int64_t n = a.n_q * a.heads, row = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+  const int d = (int)(threadIdx.x % LANES) * 4;
   if (row >= n) return;
+  const float* lse = a.part_lse + row;
+  const float* part = a.part + row * a.dim + d;
   float top = -OC_INF;
-  for (int s = 0; s < a.n_split; ++s) top = fmaxf(top, a.part_lse[s * n + row]);
+#pragma unroll 8
+  for (int s = 0; s < a.n_split; ++s) top = fmaxf(top, lse[s * n]);
   const float base = top == -OC_INF ? 0.f : top;
   float total = 0.f;
-  for (int s = 0; s < a.n_split; ++s) total += __expf(a.part_lse[s * n + row] - base);
+  f32x4 x = {0, 0, 0, 0};
+#pragma unroll 8
+  for (int s = 0; s < a.n_split; ++s) {
+    const float w = __builtin_amdgcn_exp2f((lse[s * n] - base) * kLog2e);
+    total += w;
+    if (d < a.dim) x += w * *(const f32x4*)(part + s * n * a.dim);
+  }
   const float f = total > 0.f || total != total ? 1.f / total : 0.f;
-  if (lane() == 0) a.lse[row] = total == 0.f ? -OC_INF : base + __logf(total);
-  for (int d = lane(); d < a.dim; d += 64) {
-    float x = 0.f;
-    for (int s = 0; s < a.n_split; ++s) {
-      const float w = __expf(a.part_lse[s * n + row] - base);
-      if (w != 0.f) x += w * a.part[(s * n + row) * a.dim + d];
-    }
-    ((T*)a.out)[row * a.dim + d] = (T)(x * f);
+  if (d == 0) a.lse[row] = total == 0.f ? -OC_INF : base + __logf(total);
+  if (d < a.dim) {
+    using V = __attribute__((ext_vector_type(4))) T;
+    *(V*)((T*)a.out + row * a.dim + d) = __builtin_convertvector(x * f, V);
   }
 }
 
@@ -588,41 +671,19 @@ __global__ __launch_bounds__(256) void k_attention_join(AttnArgs a) {
 // Gradients
 // ---------------------------------------------------------------------------
 
-// Per row: delta = sum_d dout out, and lse in base 2 (infinite where the row
-// sees no key, so that its probabilities come out zero).  16 lanes per row.
-template <class T>
-__global__ __launch_bounds__(256) void k_attention_delta(AttnArgs a) {
-  const int64_t row = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4), n = a.n_q * a.heads;
-  if (row >= n) return;
-  const T* x = (const T*)a.out + row * a.dim;
-  const T* y = (const T*)a.dout + row * a.dim;
-  constexpr int kPer = 16 / (int)sizeof(T);
-  using V = __attribute__((ext_vector_type(kPer))) T;
-  float sum = 0.f;
-  for (int d = (int)(threadIdx.x & 15) * kPer; d < a.dim; d += 16 * kPer) {
-    const V u = *(const V*)(x + d), v = *(const V*)(y + d);
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) sum += (float)u[i] * (float)v[i];
-  }
-#pragma unroll
-  for (int i = 8; i; i >>= 1) sum += __shfl_xor(sum, i, 16);
-  if ((threadIdx.x & 15) == 0) {
-    a.delta[row] = sum;
-    const float lse = a.lse[row];
-    a.lse2[row] = lse == -OC_INF ? OC_INF : lse * kLog2e;
-  }
-}
-
 // dQ: waves of 32 packed rows over the keys, as the forward pass.
-//   S^T = K Q^T, dP^T = V dO^T, dS^T = P^T (dP^T - delta), dQ^T += K^T dS^T.
+//   S^T = K Q^T, dP^T = V dO^T, dS^T = P^T (dP^T - delta), dQ^T += K^T dS^T,
+// with delta = sum_d dO out per row.  For the kernel of dK and dV, which runs
+// next, it leaves delta, and lse in base 2 (infinite where the row sees no
+// key, so that its probabilities come out zero).
 template <class T, int D, int NW, int BN>
 __global__ __launch_bounds__(NW * 64, (Plan<T, D>::kDqWaves)) void k_attention_dq(AttnArgs a) {
   using L = Tile<T, D, BN>;
   constexpr int NT = NW * 64, BM = NW * 32;
   __shared__ __attribute__((aligned(16))) char lds[2][2][L::kBytes];
-  const int kvh = (int)(blockIdx.x % (unsigned)a.kv_heads);
-  const Place p = place_of(a.q_off, a.n_seq, a.n_q, a.group, BM, blockIdx.x / (unsigned)a.kv_heads,
-                           gridDim.x / (unsigned)a.kv_heads);
+  const Item item(a);
+  const int kvh = item.kvh;
+  const Place p = place_of(a.q_off, a.n_seq, a.n_q, a.group, BM, item.tile, item.tiles);
   if (p.s < 0) return;
   const Seq e = seq_of(a, p.s);
   const int rows = e.lq * a.group;
@@ -633,7 +694,7 @@ __global__ __launch_bounds__(NW * 64, (Plan<T, D>::kDqWaves)) void k_attention_d
   int t0 = 0, t1 = (seen_keys(a, e, last) + BN - 1) / BN;
   if (a.n_split > 1) {
     const int per = (t1 + a.n_split - 1) / a.n_split;
-    t0 = (int)blockIdx.y * per;
+    t0 = item.part * per;
     t1 = t0 + per < t1 ? t0 + per : t1;
   }
 
@@ -656,7 +717,21 @@ __global__ __launch_bounds__(NW * 64, (Plan<T, D>::kDqWaves)) void k_attention_d
     qf[i] = global_frag<T>(qp, true, 16 * i, a.dim);
     df[i] = global_frag<T>(dp, true, 16 * i, a.dim);
   }
-  const float lse2 = a.lse2[at], delta = a.delta[at];
+  const T* op = (const T*)a.out + at * a.dim;
+  float delta = 0.f;
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i) {
+    const frag_t<T> of = global_frag<T>(op, true, 16 * i, a.dim);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) delta += (float)of[j] * (float)df[i][j];
+  }
+  delta = half_sum(delta);
+  float lse2 = a.lse[at];
+  lse2 = lse2 == -OC_INF ? OC_INF : lse2 * kLog2e;
+  if (item.part == 0 && h == 0 && r < rows) {
+    a.delta[at] = delta;
+    a.lse2[at] = lse2;
+  }
   f32x16 g[D / 32];
 #pragma unroll
   for (int d = 0; d < D / 32; ++d) g[d] = zero16();
@@ -670,7 +745,9 @@ __global__ __launch_bounds__(NW * 64, (Plan<T, D>::kDqWaves)) void k_attention_d
   };
   if (t0 < t1) load(t0, 0);
   wait_copies();
+  typename L::Lanes ln;
   for (int t = t0; t < t1; ++t) {
+    ln.renew();
     const char* kt = lds[(t - t0) & 1][0];
     const char* vt = lds[(t - t0) & 1][1];
     if (t + 1 < t1) load(t + 1, (t + 1 - t0) & 1);
@@ -679,9 +756,9 @@ __global__ __launch_bounds__(NW * 64, (Plan<T, D>::kDqWaves)) void k_attention_d
       for (int n = 0; n < BN / 32; ++n) {
         f32x16 x = zero16(), y = zero16();
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i) x = mma(L::rows(kt, 32 * n, 16 * i), qf[i], x);
+        for (int i = 0; i < D / 16; ++i) x = mma(L::rows(kt, ln, 32 * n, 16 * i), qf[i], x);
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i) y = mma(L::rows(vt, 32 * n, 16 * i), df[i], y);
+        for (int i = 0; i < D / 16; ++i) y = mma(L::rows(vt, ln, 32 * n, 16 * i), df[i], y);
         const bool mask = t * BN + 32 * n + 32 > seen_min;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
@@ -694,7 +771,7 @@ __global__ __launch_bounds__(NW * 64, (Plan<T, D>::kDqWaves)) void k_attention_d
         for (int j = 0; j < 2; ++j) {
           const frag_t<T> sf = to_frag<T>(x, 8 * j);
 #pragma unroll
-          for (int d = 0; d < D / 32; ++d) g[d] = mma(L::cols(kt, 32 * n + 16 * j, 32 * d), sf, g[d]);
+          for (int d = 0; d < D / 32; ++d) g[d] = mma(L::cols(kt, ln, 32 * n + 16 * j, 32 * d), sf, g[d]);
         }
       }
     }
@@ -704,7 +781,7 @@ __global__ __launch_bounds__(NW * 64, (Plan<T, D>::kDqWaves)) void k_attention_d
 #pragma unroll
     for (int d = 0; d < D / 32; ++d) {
       if (a.n_split > 1)
-        store_col<float>(a.part + (blockIdx.y * a.n_q * a.heads + at) * a.dim, g[d], 32 * d, a.dim, a.scale);
+        store_col<float>(a.part + (item.part * a.n_q * a.heads + at) * a.dim, g[d], 32 * d, a.dim, a.scale);
       else
         store_col<T>((T*)a.dq + at * a.dim, g[d], 32 * d, a.dim, a.scale);
     }
@@ -722,9 +799,9 @@ __global__ __launch_bounds__(NW * 64, (Plan<T, D>::kDkvWaves)) void k_attention_
   using LK = Tile<T, D, BK>;
   constexpr bool kLds = Plan<T, D>::kValuesInLds;
   __shared__ __attribute__((aligned(16))) char vt[kLds ? LK::kBytes : 16];
-  const int kvh = (int)(blockIdx.x % (unsigned)a.kv_heads);
-  const Place p = place_of(a.k_off, a.n_seq, a.n_k, 1, BK, blockIdx.x / (unsigned)a.kv_heads,
-                           gridDim.x / (unsigned)a.kv_heads);
+  const Item item(a);
+  const int kvh = item.kvh;
+  const Place p = place_of(a.k_off, a.n_seq, a.n_k, 1, BK, item.tile, item.tiles);
   if (p.s < 0) return;
   const Seq e = seq_of(a, p.s);
   // Early keys are seen by the most rows.
@@ -740,7 +817,7 @@ __global__ __launch_bounds__(NW * 64, (Plan<T, D>::kDkvWaves)) void k_attention_
   int t0 = q_first * a.group / BQ, t1 = (rows + BQ - 1) / BQ;
   if (a.n_split > 1) {
     const int per = (t1 - t0 + a.n_split - 1) / a.n_split;
-    t0 += (int)blockIdx.y * per;
+    t0 += item.part * per;
     t1 = t0 + per < t1 ? t0 + per : t1;
   }
 
@@ -788,7 +865,11 @@ __global__ __launch_bounds__(NW * 64, (Plan<T, D>::kDkvWaves)) void k_attention_
     store(0);
   }
   wait_copies();
+  typename L::Lanes ln;
+  typename LK::Lanes lk;
   for (int t = t0; t < t1; ++t) {
+    ln.renew();
+    lk.renew();
     const int b = (t - t0) & 1;
     const char* qt = lds[b][0];
     const char* dt = lds[b][1];
@@ -797,13 +878,13 @@ __global__ __launch_bounds__(NW * 64, (Plan<T, D>::kDkvWaves)) void k_attention_
     for (int n = 0; n < BQ / 32; ++n) {
       f32x16 x = zero16(), y = zero16();
 #pragma unroll
-      for (int i = 0; i < D / 16; ++i) x = mma(L::rows(qt, 32 * n, 16 * i), kf[i], x);
+      for (int i = 0; i < D / 16; ++i) x = mma(L::rows(qt, ln, 32 * n, 16 * i), kf[i], x);
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) {
         frag_t<T> f;
-        if constexpr (kLds) f = LK::rows(vt, 32 * w, 16 * i);
+        if constexpr (kLds) f = LK::rows(vt + LK::row_offset(32) * w, lk, 0, 16 * i);
         else f = vf[i];
-        y = mma(L::rows(dt, 32 * n, 16 * i), f, y);
+        y = mma(L::rows(dt, ln, 32 * n, 16 * i), f, y);
       }
       const int rn = t * BQ + 32 * n;
       // The tile's first row sees the fewest keys.
@@ -821,9 +902,9 @@ __global__ __launch_bounds__(NW * 64, (Plan<T, D>::kDkvWaves)) void k_attention_
       for (int j = 0; j < 2; ++j) {
         const frag_t<T> pf = to_frag<T>(x, 8 * j), sf = to_frag<T>(y, 8 * j);
 #pragma unroll
-        for (int d = 0; d < D / 32; ++d) gv[d] = mma(L::cols(dt, 32 * n + 16 * j, 32 * d), pf, gv[d]);
+        for (int d = 0; d < D / 32; ++d) gv[d] = mma(L::cols(dt, ln, 32 * n + 16 * j, 32 * d), pf, gv[d]);
 #pragma unroll
-        for (int d = 0; d < D / 32; ++d) gk[d] = mma(L::cols(qt, 32 * n + 16 * j, 32 * d), sf, gk[d]);
+        for (int d = 0; d < D / 32; ++d) gk[d] = mma(L::cols(qt, ln, 32 * n + 16 * j, 32 * d), sf, gk[d]);
       }
     }
     if (t + 1 < t1) store((t + 1 - t0) & 1);
@@ -834,8 +915,8 @@ __global__ __launch_bounds__(NW * 64, (Plan<T, D>::kDkvWaves)) void k_attention_
 #pragma unroll
     for (int d = 0; d < D / 32; ++d) {
       if (a.n_split > 1) {
-        store_col<float>(a.part + (2 * blockIdx.y) * n + at, gk[d], 32 * d, a.dim, a.scale);
-        store_col<float>(a.part + (2 * blockIdx.y + 1) * n + at, gv[d], 32 * d, a.dim, kDown);
+        store_col<float>(a.part + (2 * item.part) * n + at, gk[d], 32 * d, a.dim, a.scale);
+        store_col<float>(a.part + (2 * item.part + 1) * n + at, gv[d], 32 * d, a.dim, kDown);
       } else {
         store_col<T>((T*)a.dk + at, gk[d], 32 * d, a.dim, a.scale);
         store_col<T>((T*)a.dv + at, gv[d], 32 * d, a.dim, kDown);
@@ -844,16 +925,17 @@ __global__ __launch_bounds__(NW * 64, (Plan<T, D>::kDkvWaves)) void k_attention_
   }
 }
 
-// out = the sum of `parts` arrays of n, `stride` apart, in order; four
-// elements a thread.
+// Output blockIdx.y of two = the sum of `parts` arrays of n, gridDim.y n
+// apart, in order; four elements a thread.
 template <class T>
-__global__ __launch_bounds__(256) void k_sum_parts(const float* part, int64_t n, int64_t stride, int parts, T* out) {
+__global__ __launch_bounds__(256) void k_sum_parts(const float* part, int64_t n, int parts, T* out0, T* out1) {
   const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
   if (at >= n) return;
-  f32x4 x = *(const f32x4*)(part + at);
-  for (int s = 1; s < parts; ++s) x += *(const f32x4*)(part + s * stride + at);
+  const float* p = part + blockIdx.y * n + at;
+  f32x4 x = *(const f32x4*)p;
+  for (int s = 1; s < parts; ++s) x += *(const f32x4*)(p + (int64_t)s * gridDim.y * n);
   using V = __attribute__((ext_vector_type(4))) T;
-  *(V*)(out + at) = __builtin_convertvector(x, V);
+  *(V*)((blockIdx.y ? out1 : out0) + at) = __builtin_convertvector(x, V);
 }
 
 // ---------------------------------------------------------------------------
@@ -927,18 +1009,22 @@ hipError_t launch_attention(const AttnArgs& a, int dtype, hipStream_t s) {
     const hipError_t err = by_dim(a.dim, [&](auto d) {
       constexpr int D = decltype(d)::value;
       k_attention<T, D, 1, kWaves, Plan<T, D>::kKeys>
-          <<<dim3((unsigned)workgroups, (unsigned)a.n_split), kWaves * 64, 0, s>>>(a);
+          <<<(unsigned)(workgroups * a.n_split), kWaves * 64, 0, s>>>(a);
       return hipGetLastError();
     });
     if (err != hipSuccess || a.n_split == 1) return err;
-    k_attention_join<T><<<(unsigned)((a.n_q * a.heads + 3) / 4), 256, 0, s>>>(a);
+    const int64_t n = a.n_q * a.heads;
+    if (a.dim <= 64)
+      k_attention_join<T, 16><<<(unsigned)((n + 15) / 16), 256, 0, s>>>(a);
+    else
+      k_attention_join<T, 32><<<(unsigned)((n + 7) / 8), 256, 0, s>>>(a);
     return hipGetLastError();
   });
 }
 
 template <class T>
-static hipError_t sum_parts(const float* part, int64_t n, int64_t stride, int parts, void* out, hipStream_t s) {
-  k_sum_parts<T><<<(unsigned)((n / 4 + 255) / 256), 256, 0, s>>>(part, n, stride, parts, (T*)out);
+static hipError_t sum_parts(const float* part, int64_t n, int parts, void* out0, void* out1, hipStream_t s) {
+  k_sum_parts<T><<<dim3((unsigned)((n / 4 + 255) / 256), out1 ? 2 : 1), 256, 0, s>>>(part, n, parts, (T*)out0, (T*)out1);
   return hipGetLastError();
 }
 
@@ -948,18 +1034,16 @@ hipError_t launch_attention_backward(AttnArgs a, int dtype, hipStream_t s) {
     using T = decltype(t);
     hipError_t err = hipSuccess;
     if (a.n_q > 0) {
-      k_attention_delta<T><<<(unsigned)((a.n_q * a.heads + 15) / 16), 256, 0, s>>>(a);
-      if ((err = hipGetLastError()) != hipSuccess) return err;
       a.n_split = parts.dq;
       err = by_dim(a.dim, [&](auto d) {
         constexpr int D = decltype(d)::value;
         const int64_t workgroups = slots_of(a.n_q * a.group, kTile, a.n_seq) * a.kv_heads;
         k_attention_dq<T, D, kWaves, Plan<T, D>::kDqKeys>
-            <<<dim3((unsigned)workgroups, (unsigned)a.n_split), kWaves * 64, 0, s>>>(a);
+            <<<(unsigned)(workgroups * a.n_split), kWaves * 64, 0, s>>>(a);
         return hipGetLastError();
       });
       const int64_t n = a.n_q * a.heads * a.dim;
-      if (err == hipSuccess && parts.dq > 1) err = sum_parts<T>(a.part, n, n, parts.dq, a.dq, s);
+      if (err == hipSuccess && parts.dq > 1) err = sum_parts<T>(a.part, n, parts.dq, a.dq, nullptr, s);
       if (err != hipSuccess) return err;
     }
     if (a.n_k > 0) {
@@ -968,12 +1052,11 @@ hipError_t launch_attention_backward(AttnArgs a, int dtype, hipStream_t s) {
         constexpr int D = decltype(d)::value;
         const int64_t workgroups = slots_of(a.n_k, kTile, a.n_seq) * a.kv_heads;
         k_attention_dkv<T, D, kWaves, Plan<T, D>::kDkvRows>
-            <<<dim3((unsigned)workgroups, (unsigned)a.n_split), kWaves * 64, 0, s>>>(a);
+            <<<(unsigned)(workgroups * a.n_split), kWaves * 64, 0, s>>>(a);
         return hipGetLastError();
       });
       const int64_t n = a.n_k * a.kv_heads * a.dim;
-      if (err == hipSuccess && parts.dkv > 1) err = sum_parts<T>(a.part, n, 2 * n, parts.dkv, a.dk, s);
-      if (err == hipSuccess && parts.dkv > 1) err = sum_parts<T>(a.part + n, n, 2 * n, parts.dkv, a.dv, s);
+      if (err == hipSuccess && parts.dkv > 1) err = sum_parts<T>(a.part, n, parts.dkv, a.dk, a.dv, s);
     }
     return err;
   });
