@@ -93,6 +93,20 @@ __device__ __forceinline__ f32x16 zero16() {
   return z;
 }
 
+// Order for the scheduler: `AHEAD` LDS reads, then PRODUCTS times a matrix
+// product and READS more of them, then LAST products.  Left to itself it
+// waits for each fragment just before the product that takes it.
+template <int AHEAD, int PRODUCTS, int READS, int LAST>
+__device__ __forceinline__ void pace() {
+  if constexpr (AHEAD > 0) __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
+#pragma unroll
+  for (int i = 0; i < PRODUCTS; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+  }
+  if constexpr (LAST > 0) __builtin_amdgcn_sched_group_barrier(0x8, LAST, 0);
+}
+
 // The eight accumulator values from `first` on as a fragment.
 template <class T>
 __device__ __forceinline__ frag_t<T> to_frag(const f32x16& c, int first) {
@@ -547,18 +561,8 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention(AttnArgs a) {
           for (int m = 0; m < MT; ++m) x[m][n] = mma(kf, qf[m][i], x[m][n]);
         }
       }
-      if constexpr (sizeof(T) == 2 && D > 64) {
-        // Four fragments ahead of the product that takes them (907 to 924
-        // TFLOP/s at head size 128; smaller ones have too few to gain).
-        constexpr int N = BN / 32 * (D / 16);
-        __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
-#pragma unroll
-        for (int i = 0; i < N - 4; ++i) {
-          __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-        }
-        __builtin_amdgcn_sched_group_barrier(0x8, 4, 0);
-      }
+      // 907 to 924 TFLOP/s at head size 128; smaller ones gain nothing.
+      if constexpr (sizeof(T) == 2 && D > 64) pace<4, BN / 32 * (D / 16) - 4, 1, 4>();
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
         if ((t + 1) * BN > seen_min[m]) {
@@ -567,7 +571,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention(AttnArgs a) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
               const int key = t * BN + 32 * n + 8 * (i / 4) + 4 * h + i % 4;
-              if (key >= seen[m]) x[m][n][i] = -OC_INF;
+              x[m][n][i] = key >= seen[m] ? -OC_INF : x[m][n][i];
             }
         }
         float top = x[m][0][0];
@@ -759,13 +763,15 @@ __global__ __launch_bounds__(NW * 64, (Plan<T, D>::kDqWaves)) void k_attention_d
         for (int i = 0; i < D / 16; ++i) x = mma(L::rows(kt, ln, 32 * n, 16 * i), qf[i], x);
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) y = mma(L::rows(vt, ln, 32 * n, 16 * i), df[i], y);
-        const bool mask = t * BN + 32 * n + 32 > seen_min;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int key = t * BN + 32 * n + 8 * (i / 4) + 4 * h + i % 4;
-          const float pr = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], c, -lse2));
-          x[i] = pr * (y[i] - delta);
-          if (mask && key >= seen) x[i] = 0.f;
+        for (int i = 0; i < 16; ++i)
+          x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], c, -lse2)) * (y[i] - delta);
+        if (t * BN + 32 * n + 32 > seen_min) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int key = t * BN + 32 * n + 8 * (i / 4) + 4 * h + i % 4;
+            x[i] = key >= seen ? 0.f : x[i];
+          }
         }
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -795,7 +801,7 @@ __global__ __launch_bounds__(NW * 64, (Plan<T, D>::kDkvWaves)) void k_attention_
   using L = Tile<T, D, BQ>;
   constexpr int NT = NW * 64, BK = NW * 32;
   __shared__ __attribute__((aligned(16))) char lds[2][2][L::kBytes];
-  __shared__ float stat[2][2][BQ];
+  __shared__ __attribute__((aligned(16))) float stat[2][2][BQ];
   using LK = Tile<T, D, BK>;
   constexpr bool kLds = Plan<T, D>::kValuesInLds;
   __shared__ __attribute__((aligned(16))) char vt[kLds ? LK::kBytes : 16];
@@ -886,18 +892,35 @@ __global__ __launch_bounds__(NW * 64, (Plan<T, D>::kDkvWaves)) void k_attention_
         else f = vf[i];
         y = mma(L::rows(dt, ln, 32 * n, 16 * i), f, y);
       }
-      const int rn = t * BQ + 32 * n;
-      // The tile's first row sees the fewest keys.
-      const bool mask = a.causal && seen_keys(a, e, rn) < j0 + w * 32 + 32;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int rr = 8 * (i / 4) + 4 * h + i % 4;
-        float pr = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], c, -stat[b][0][32 * n + rr]));
-        float g = pr * __builtin_fmaf(y[i], kDown, -stat[b][1][32 * n + rr]);
-        if (mask && key >= seen_keys(a, e, rn + rr)) pr = g = 0.f;
-        x[i] = pr;
-        y[i] = g;
+      // The three phases apart, or the scheduler stretches fragments over more
+      // of them than there are registers for (at head size 128, 13 spilled: 645
+      // TFLOP/s in five products, 725 without; head size 64 526 to 630).
+      if constexpr (sizeof(T) == 2 && D > 32) {
+        pace<4, D / 16, 1, 0>();
+        pace<0, kLds ? D / 16 - 2 : D / 16 - 4, kLds ? 2 : 1, kLds ? 2 : 4>();
       }
+      if constexpr (D > 32) __builtin_amdgcn_sched_barrier(0);
+      const int rn = t * BQ + 32 * n;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const f32x4 lse2 = *(const f32x4*)&stat[b][0][32 * n + 8 * j + 4 * h];
+        const f32x4 delta = *(const f32x4*)&stat[b][1][32 * n + 8 * j + 4 * h];
+#pragma unroll
+        for (int i = 4 * j; i < 4 * j + 4; ++i) {
+          x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], c, -lse2[i % 4]));
+          y[i] = x[i] * __builtin_fmaf(y[i], kDown, -delta[i % 4]);
+        }
+      }
+      // The tile's first row sees the fewest keys.
+      if (a.causal && seen_keys(a, e, rn) < j0 + w * 32 + 32) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const bool hide = key >= seen_keys(a, e, rn + 8 * (i / 4) + 4 * h + i % 4);
+          x[i] = hide ? 0.f : x[i];
+          y[i] = hide ? 0.f : y[i];
+        }
+      }
+      if constexpr (D > 32) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         const frag_t<T> pf = to_frag<T>(x, 8 * j), sf = to_frag<T>(y, 8 * j);
