@@ -1,0 +1,178 @@
+"""A small network over whole samples: attention between the leaves of a grid-octree.
+
+The convolutions mix neighbours; here every leaf of a sample sees every other
+one (or, causal, those before it in the leaf order).  The leaf rows of a batch
+are one packed array with a sequence per sample, so that the structure's
+prefix gives the offsets and nothing is padded:
+
+  h0 = x W_in                                          float stream
+  a  = norm(h0) w1;  q, k, v = a W_qkv;  o = attention(q, k, v)
+  h1 = h0 + o W_o;   c = norm(h1) w2                   one call
+  logits = c W_cls;  loss = -mean log p(label) over labelled leaves
+
+The stream is float, the branches bfloat16.  train_step() runs it forward and
+backward, clips the gradients by their global norm and steps; LeafCache serves
+a causal block row by row.  The plain products with the weights are torch's.
+
+  python -m paper_1611_05009_amd.leaf_block --steps 20
+"""
+from __future__ import annotations
+
+import argparse
+from dataclasses import dataclass
+
+import numpy as np
+import torch
+
+from . import octnet as oc
+from . import synth
+
+BRANCH = torch.bfloat16
+
+
+@dataclass
+class Scene:
+    """Leaves of a labelled point cloud at a coarse resolution."""
+
+    g: oc.Octree
+    x: torch.Tensor        # float32 [n_leaves, features]
+    labels: torch.Tensor   # int32 [n_leaves], -1: none
+    offsets: torch.Tensor  # int64 [n + 1]
+
+
+def scene(batch: int = 2, shrink: int = 8, device: str = "cuda") -> Scene:
+    """Facade point clouds of the U-Net workload, mapped into octrees of 256 /
+    shrink voxels a side: mean point features and majority label per leaf."""
+    wl = synth.WORKLOADS["unet"]
+    pts, bidx, feat, labels = (torch.from_numpy(np.ascontiguousarray(t)).to(device) for t in synth.point_cloud(wl, batch=batch))
+    pts = pts / shrink
+    gd = wl.grid // shrink
+    g = oc.build(oc.points_voxelize(pts, batch, gd, gd, gd, batch=bidx))
+    rows = oc.points_leaf_rows(g, pts, bidx)
+    return Scene(g, oc.points_average(g, rows, feat), oc.points_vote(g, rows, labels.int(), int(labels.max()) + 1),
+                 oc.leaf_offsets(g))
+
+
+class LeafBlock:
+    def __init__(self, features: int, width: int, heads: int, kv_heads: int, classes: int, causal: bool = False,
+                 seed: int = 0, device: str = "cuda"):
+        if width % heads:
+            raise ValueError("width must be a multiple of heads")
+        self.heads, self.kv_heads, self.dim = heads, kv_heads, width // heads
+        self.causal = causal
+        gen = torch.Generator().manual_seed(seed)
+
+        def weight(a, b):
+            return (torch.randn(a, b, generator=gen) / a ** 0.5).to(device)
+
+        total = (heads + 2 * kv_heads) * self.dim
+        self.params = {"w_in": weight(features, width), "w_qkv": weight(width, total), "w_o": weight(width, width),
+                       "w_cls": weight(width, classes), "w1": torch.ones(width, device=device),
+                       "w2": torch.ones(width, device=device)}
+
+    def _split(self, qkv: torch.Tensor):
+        """Queries, keys and values as slices of the projection's output."""
+        t = qkv.view(qkv.shape[0], self.heads + 2 * self.kv_heads, self.dim)
+        return t[:, :self.heads], t[:, self.heads:self.heads + self.kv_heads], t[:, self.heads + self.kv_heads:]
+
+    def forward(self, x: torch.Tensor, offsets: torch.Tensor | None, keep: dict | None = None) -> torch.Tensor:
+        """Logits (bfloat16) of leaf features x; `keep` receives what backward needs."""
+        p = {k: w.to(BRANCH) if w.dim() == 2 else w for k, w in self.params.items()}
+        h0 = x @ self.params["w_in"]
+        a, _ = oc.rms_norm(h0, p["w1"], out_dtype=BRANCH)
+        q, k, v = self._split(a @ p["w_qkv"])
+        o, lse = oc.attention(q, k, v, q_offsets=offsets, k_offsets=offsets, causal=self.causal)
+        c, h1 = oc.rms_norm(o.flatten(1) @ p["w_o"], p["w2"], residual=h0)
+        logits = c @ p["w_cls"]
+        if keep is not None:
+            keep.update(p=p, x=x, h0=h0, a=a, q=q, k=k, v=v, o=o, lse=lse, h1=h1, c=c, logits=logits)
+        return logits
+
+    def backward(self, keep: dict, offsets: torch.Tensor | None, dlogits: torch.Tensor) -> dict:
+        """Gradients of the parameters, in float32."""
+        p = keep["p"]
+        o2 = keep["o"].flatten(1)
+        g = {"w_cls": (keep["c"].T @ dlogits).float()}
+        dh1, g["w2"] = oc.rms_norm_backward(keep["h1"], p["w2"], dlogits @ p["w_cls"].T)
+        db = dh1.to(BRANCH)
+        g["w_o"] = (o2.T @ db).float()
+        do = (db @ p["w_o"].T).view_as(keep["o"])
+        dqkv = torch.cat(oc.attention_backward(keep["q"], keep["k"], keep["v"], keep["o"], keep["lse"], do,
+                                               q_offsets=offsets, k_offsets=offsets, causal=self.causal), dim=1).flatten(1)
+        g["w_qkv"] = (keep["a"].T @ dqkv).float()
+        dh0, g["w1"] = oc.rms_norm_backward(keep["h0"], p["w1"], dqkv @ p["w_qkv"].T, dsum=dh1)
+        g["w_in"] = keep["x"].T @ dh0
+        return g
+
+    def loss_and_grads(self, s: Scene):
+        """(mean loss over labelled leaves, gradients, what label_logprobs returned)."""
+        keep = {}
+        logits = self.forward(s.x, s.offsets, keep)
+        lp = oc.label_logprobs(logits, s.labels, top=1)
+        n = (s.labels >= 0).sum().clamp(min=1)
+        dlogits = oc.label_logprobs_backward(logits, s.labels, lp.lse, (-1.0 / n).expand(s.x.shape[0]).contiguous())
+        return -lp.logprob.sum() / n, self.backward(keep, s.offsets, dlogits), lp
+
+    def train_step(self, s: Scene, lr: float = 0.05, max_norm: float = 1.0):
+        """One step; (loss, gradient norm, share of labelled leaves whose
+        likeliest label is theirs), all on the GPU."""
+        loss, grads, lp = self.loss_and_grads(s)
+        norm = oc.clip_grad_norm(list(grads.values()), max_norm)
+        for k, w in self.params.items():
+            w.sub_(grads[k], alpha=lr)
+        has = s.labels >= 0
+        right = ((lp.top_label[:, 0] == s.labels) & has).sum() / has.sum().clamp(min=1)
+        return loss, norm, right
+
+
+class LeafCache:
+    """Keys and values of a causal block's rows so far, for `n` sequences of up
+    to `capacity` rows: each call brings the same number of new rows to every
+    sequence and returns their logits."""
+
+    def __init__(self, block: LeafBlock, n: int, capacity: int):
+        if not block.causal:
+            raise ValueError("only a causal block can be served row by row")
+        dev = block.params["w1"].device
+        self.block, self.n, self.capacity, self.used = block, n, capacity, 0
+        self.k = torch.zeros((n, capacity, block.kv_heads, block.dim), dtype=BRANCH, device=dev)
+        self.v = torch.zeros_like(self.k)
+        self.k_offsets = torch.arange(n + 1, device=dev) * capacity
+
+    def extend(self, x: torch.Tensor) -> torch.Tensor:
+        """Logits [n, rows, classes] of features x [n, rows, features]."""
+        b, p = self.block, {k: w.to(BRANCH) if w.dim() == 2 else w for k, w in self.block.params.items()}
+        n, rows = x.shape[:2]
+        if n != self.n or self.used + rows > self.capacity:
+            raise ValueError("the cache holds %d rows of %d sequences" % (self.capacity, self.n))
+        h0 = x.reshape(n * rows, -1) @ b.params["w_in"]
+        a, _ = oc.rms_norm(h0, p["w1"], out_dtype=BRANCH)
+        q, k, v = b._split(a @ p["w_qkv"])
+        self.k[:, self.used:self.used + rows] = k.reshape(n, rows, b.kv_heads, b.dim)
+        self.v[:, self.used:self.used + rows] = v.reshape(n, rows, b.kv_heads, b.dim)
+        self.used += rows
+        lengths = torch.full((n,), self.used, dtype=torch.int64, device=x.device)
+        q_offsets = torch.arange(n + 1, device=x.device) * rows
+        o, _ = oc.attention(q, self.k.flatten(0, 1), self.v.flatten(0, 1), q_offsets=q_offsets, k_offsets=self.k_offsets,
+                            k_lengths=lengths, causal=True)
+        c, _ = oc.rms_norm(o.flatten(1) @ p["w_o"], p["w2"], residual=h0)
+        return (c @ p["w_cls"]).view(n, rows, -1)
+
+
+def main():
+    ap = argparse.ArgumentParser(description="train a leaf block on synthetic facades")
+    ap.add_argument("--steps", type=int, default=20)
+    ap.add_argument("--batch", type=int, default=2)
+    ap.add_argument("--width", type=int, default=128)
+    a = ap.parse_args()
+    s = scene(a.batch)
+    classes = int(s.labels.max()) + 1
+    block = LeafBlock(s.x.shape[1], a.width, heads=4, kv_heads=2, classes=classes)
+    print("%d leaves of %d samples, %d classes" % (s.x.shape[0], a.batch, classes))
+    for i in range(a.steps):
+        loss, norm, right = block.train_step(s)
+        print("step %d: loss %.4f, gradient norm %.4f, %.1f%% right" % (i, float(loss), float(norm), 100 * float(right)))
+
+
+if __name__ == "__main__":
+    main()

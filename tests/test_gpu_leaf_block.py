@@ -1,0 +1,95 @@
+"""The leaf block (norm, attention, label log probabilities, clipping chained)
+against the same network in 64-bit torch, and its cache against whole calls."""
+import math
+
+import pytest
+import torch
+
+from common import log
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+
+
+def plain_loss(block, params, x, offsets, labels):
+    """The network's loss by autograd in float64, weights as the branches
+    round them."""
+    def norm(h, w):
+        return h / (h.square().mean(1, keepdim=True) + 1e-6).sqrt() * w
+
+    h0 = x @ params["w_in"]
+    qkv = (norm(h0, params["w1"]) @ params["w_qkv"]).view(-1, block.heads + 2 * block.kv_heads, block.dim)
+    group = block.heads // block.kv_heads
+    out = []
+    for a, b in zip(offsets, offsets[1:]):
+        rows = []
+        for h in range(block.heads):
+            q = qkv[a:b, h]
+            k = qkv[a:b, block.heads + h // group]
+            v = qkv[a:b, block.heads + block.kv_heads + h // group]
+            s = q @ k.T / math.sqrt(block.dim)
+            if block.causal:
+                s = s.masked_fill(torch.ones_like(s, dtype=torch.bool).triu(1), -math.inf)
+            rows.append(torch.softmax(s, 1) @ v)
+        out.append(torch.stack(rows, 1))
+    h1 = h0 + torch.cat(out).flatten(1) @ params["w_o"]
+    lp = torch.log_softmax(norm(h1, params["w2"]) @ params["w_cls"], 1)
+    has = labels >= 0
+    return -lp[has].gather(1, labels[has].long()[:, None]).mean()
+
+
+@pytest.mark.parametrize("causal", [False, True])
+def test_gradients(causal):
+    """The branches round to bfloat16 (unit 2^-8) about a dozen times between
+    the input and a gradient: with independent roundings the relative error of
+    a gradient as a whole is of order sqrt(12) 2^-9 = 0.7%; the bar is 2^-5."""
+    from paper_1611_05009_amd import leaf_block as lb
+    s = lb.scene(batch=2, shrink=16)
+    block = lb.LeafBlock(s.x.shape[1], 64, heads=4, kv_heads=2, classes=8, causal=causal, seed=3)
+    loss, grads, _ = block.loss_and_grads(s)
+    params = {k: (w.to(torch.bfloat16) if w.dim() == 2 and k != "w_in" else w).double().cpu().requires_grad_() for k, w in block.params.items()}
+    want = plain_loss(block, params, s.x.double().cpu(), s.offsets.tolist(), s.labels.cpu())
+    want.backward()
+    log("%d leaves, loss %.5f, in 64 bits %.5f" % (s.x.shape[0], float(loss), float(want.detach())))
+    assert abs(float(loss) - float(want.detach())) <= 2.0 ** -6 * abs(float(want.detach()))
+    for k, g in grads.items():
+        w = params[k].grad
+        e = float((g.cpu().double() - w).norm() / w.norm())
+        log("  %s: relative error %.4f" % (k, e))
+        assert e <= 2.0 ** -5, k
+
+
+def test_training_learns():
+    from paper_1611_05009_amd import leaf_block as lb
+    s = lb.scene(batch=2, shrink=16)
+    block = lb.LeafBlock(s.x.shape[1], 64, heads=4, kv_heads=1, classes=8)
+    losses = [float(block.train_step(s, lr=0.1)[0]) for _ in range(30)]
+    log("loss %.4f -> %.4f" % (losses[0], losses[-1]))
+    assert losses[-1] < 0.9 * losses[0]
+
+
+def test_cache_serves_the_same_logits():
+    """Row by row and in pieces against one causal call over the whole rows.
+    Scores and sums differ in their order only; the branches' bfloat16
+    roundings then differ by a unit here and there: 2^-6 of the largest logit."""
+    from paper_1611_05009_amd import leaf_block as lb
+    n, rows, f = 3, 150, 8
+    x = torch.randn(n, rows, f, generator=torch.Generator().manual_seed(1)).cuda()
+    block = lb.LeafBlock(f, 64, heads=8, kv_heads=2, classes=8, causal=True)
+    off = torch.arange(n + 1, device="cuda") * rows
+    whole = block.forward(x.flatten(0, 1), off).view(n, rows, -1).float()
+    cache = lb.LeafCache(block, n, capacity=200)
+    got, at = [], 0
+    for step in [100] + [1] * 10 + [7, 33]:
+        got.append(cache.extend(x[:, at:at + step]))
+        at += step
+    got = torch.cat(got, 1).float()
+    assert at == rows and got.shape == whole.shape
+    assert float((got - whole).abs().max()) <= 2.0 ** -6 * float(whole.abs().max())
+    with pytest.raises(ValueError):
+        cache.extend(x[:, :60])

@@ -1,0 +1,153 @@
+"""Host-side refusals of the sequence operators: every bad argument is turned
+away before a launch, with its reason (no GPU work is issued)."""
+import ctypes
+import os
+
+import pytest
+import torch
+
+FAKE = ctypes.c_void_p(0x1000)   # never dereferenced: the checks come first
+ODD = ctypes.c_void_p(0x1002)    # not aligned to 16 bytes
+
+
+@pytest.fixture(scope="module")
+def L():
+    from paper_1611_05009_amd import octnet
+    if not os.path.exists(octnet.LIB_PATH):
+        from paper_1611_05009_amd import build_lib
+        build_lib.build()
+    return octnet.lib()
+
+
+def attention(L, back=False, **kw):
+    a = dict(q=FAKE, q_row=64, q_head=32, k=FAKE, k_row=32, k_head=32, v=FAKE, v_row=32, v_head=32, q_off=None, k_off=None,
+             k_len=None, n_seq=1, n_q=10, n_k=20, heads=2, kv_heads=1, dim=32, dtype=1, scale=1.0, causal=0, out=FAKE,
+             lse=FAKE, dout=FAKE, dq=FAKE, dk=FAKE, dv=FAKE, ws=FAKE, ws_bytes=1 << 30)
+    a.update(kw)
+    head = [a[k] for k in ("q", "q_row", "q_head", "k", "k_row", "k_head", "v", "v_row", "v_head")]
+    sizes = [a[k] for k in ("n_seq", "n_q", "n_k", "heads", "kv_heads", "dim", "dtype", "scale", "causal")]
+    if back:
+        return L.oc_attention_backward(*head, a["out"], a["lse"], a["dout"], a["q_off"], a["k_off"], *sizes, a["dq"], a["dk"],
+                                       a["dv"], a["ws"], a["ws_bytes"], None)
+    return L.oc_attention(*head, a["q_off"], a["k_off"], a["k_len"], *sizes, a["out"], a["lse"], a["ws"], a["ws_bytes"], None)
+
+
+@pytest.mark.parametrize("back", [False, True])
+@pytest.mark.parametrize("rc,kw", [
+    (-1, dict(q=None)), (-1, dict(k=None)), (-1, dict(v=None)), (-1, dict(out=None)), (-1, dict(lse=None)),
+    (-1, dict(q=ODD)), (-1, dict(v=ODD)), (-1, dict(out=ODD)),
+    (-1, dict(n_q=-1)), (-1, dict(n_k=-1)), (-1, dict(n_seq=0)), (-1, dict(n_seq=2)),       # sequences without offsets
+    (-1, dict(heads=0)), (-1, dict(kv_heads=0)), (-1, dict(heads=3, kv_heads=2)),
+    (-1, dict(dim=0)), (-1, dict(dim=12)), (-1, dict(dim=136)), (-1, dict(dtype=3)), (-1, dict(dtype=-1)),
+    (-1, dict(q_row=33)), (-1, dict(k_row=-32)), (-1, dict(v_head=4)),
+    (-1, dict(scale=0.0)), (-1, dict(scale=-1.0)), (-1, dict(scale=float("nan"))), (-1, dict(scale=float("inf"))),
+    (-5, dict(n_q=1 << 31)), (-5, dict(n_k=1 << 31)), (-5, dict(n_q=1 << 30, heads=8)), (-5, dict(q_row=1 << 33)),
+])
+def test_attention_refusals(L, back, rc, kw):
+    assert attention(L, back, **kw) == rc, L.oc_last_error()
+    assert b"oc_attention" in L.oc_last_error()
+
+
+def test_attention_workspaces(L):
+    nb = ctypes.c_size_t(7)
+    # many rows: no parts; single rows against long keys: parts
+    assert L.oc_attention_workspace(100000, 100000, 1, 8, 8, 64, ctypes.byref(nb)) == 0 and nb.value == 0
+    assert L.oc_attention_workspace(4, 40000, 4, 8, 1, 64, ctypes.byref(nb)) == 0 and nb.value > 0
+    assert attention(L, n_q=4, n_k=40000, heads=2, ws_bytes=100) == -3
+    assert attention(L, n_q=4, n_k=40000, heads=2, ws=None) == -3
+    assert attention(L, True, ws_bytes=16) == -3
+    assert attention(L, True, dout=None) == -1 and attention(L, True, dk=None) == -1
+    assert L.oc_attention_workspace(4, 4, 1, 8, 3, 64, ctypes.byref(nb)) == -1
+    assert L.oc_attention_workspace(4, 4, 1, 8, 8, 64, None) == -1
+    assert L.oc_attention_backward_workspace(4, 4, 1, 8, 8, 7, ctypes.byref(nb)) == -1
+    # nothing to do
+    assert attention(L, n_q=0, q=None, out=None, lse=None) == 0
+
+
+def test_norm_refusals(L):
+    def fwd(x=FAKE, xt=0, res=None, st=0, w=FAKE, rows=4, c=16, eps=1e-6, s=None, y=FAKE, yt=0, scale=None):
+        return L.oc_rms_norm(x, xt, res, st, w, rows, c, eps, s, y, yt, scale, None)
+
+    assert fwd(x=None) == -1 and fwd(w=None) == -1 and fwd(y=None) == -1
+    assert fwd(rows=-1) == -1 and fwd(c=0) == -1 and fwd(c=32769) == -1 and fwd(eps=-1.0) == -1
+    assert fwd(eps=float("nan")) == -1
+    assert fwd(xt=3) == -1 and fwd(xt=1, st=2, yt=1) == -1 and fwd(xt=1, st=1, yt=2) == -1 and fwd(yt=9) == -1
+    assert fwd(yt=3) == -1                       # 8 bits without a place for the scales
+    assert fwd(rows=1 << 60) == -5
+    assert fwd(rows=0, x=None) == 0
+
+    def back(s=FAKE, st=0, w=FAKE, dy=FAKE, yt=0, rows=4, c=16, dx=FAKE, dw=FAKE, ws=FAKE, nb=1 << 20):
+        return L.oc_rms_norm_backward(s, st, w, dy, yt, None, rows, c, 1e-6, dx, dw, ws, nb, None)
+
+    assert back(s=None) == -1 and back(dy=None) == -1 and back(dx=None) == -1 and back(w=None) == -1
+    assert back(st=1, yt=2) == -1 and back(st=3) == -1 and back(yt=3) == -1 and back(c=40000) == -1
+    assert back(nb=4) == -3 and back(ws=None) == -3
+    nb = ctypes.c_size_t(0)
+    assert L.oc_rms_norm_backward_workspace(100, 64, ctypes.byref(nb)) == 0 and nb.value > 0
+    assert L.oc_rms_norm_backward_workspace(100, 0, ctypes.byref(nb)) == -1
+
+
+def test_label_refusals(L):
+    def fwd(x=FAKE, dt=0, lab=FAKE, rows=4, classes=10, top=0, lp=FAKE, lse=FAKE, ent=None, tl=FAKE, ti=FAKE, ws=FAKE, nb=1 << 30):
+        return L.oc_label_logprobs(x, dt, lab, rows, classes, top, lp, lse, ent, tl, ti, ws, nb, None)
+
+    assert fwd(x=None) == -1 and fwd(lab=None) == -1 and fwd(lp=None) == -1 and fwd(lse=None) == -1
+    assert fwd(top=2, tl=None) == -1 and fwd(top=2, ti=None) == -1
+    assert fwd(top=11) == -1 and fwd(top=-1) == -1 and fwd(classes=100, top=33) == -1
+    assert fwd(rows=-1) == -1 and fwd(classes=0) == -1 and fwd(dt=3) == -1
+    assert fwd(rows=1 << 31) == -5 and fwd(classes=(1 << 29) + 1) == -5
+    nb = ctypes.c_size_t(0)
+    assert L.oc_label_logprobs_workspace(1, 200000, 4, ctypes.byref(nb)) == 0 and nb.value > 0
+    assert fwd(rows=1, classes=200000, top=4, nb=nb.value - 1) == -3
+    assert fwd(rows=1, classes=200000, top=4, ws=None) == -3
+    assert fwd(rows=0, x=None) == 0
+
+    def back(x=FAKE, lab=FAKE, lse=FAKE, g=FAKE, ent=FAKE, ge=None, d=FAKE, dt=0, classes=10):
+        return L.oc_label_logprobs_backward(x, dt, lab, 4, classes, lse, g, ent, ge, d, None)
+
+    assert back(x=None) == -1 and back(lab=None) == -1 and back(lse=None) == -1 and back(d=None) == -1
+    assert back(ent=None, ge=FAKE) == -1 and back(dt=7) == -1 and back(classes=-3) == -1
+
+
+def test_clip_refusals(L):
+    P, I64, I = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int
+    nb = ctypes.c_size_t(0)
+
+    def clip(ptrs=(0x1000,), counts=(5,), types=(0,), n=1, most=1.0, norm=FAKE, ws=FAKE, size=1 << 20):
+        return L.oc_clip_grad_norm((P * len(ptrs))(*ptrs), (P * len(ptrs))(*ptrs), (I64 * len(counts))(*counts),
+                                   (I * len(types))(*types), n, most, norm, ws, size, None)
+
+    assert clip(ptrs=(None,)) == -1 and clip(types=(3,)) == -1 and clip(counts=(-1,)) == -1 and clip(n=-1) == -1
+    assert clip(most=-1.0) == -1 and clip(most=float("nan")) == -1 and clip(norm=None) == -1
+    assert clip(ptrs=(0x1002,)) == -1            # a float array at two bytes
+    assert clip(ws=None) == -3 and clip(size=4) == -3
+    assert clip(counts=(1 << 62,)) == -5
+    assert L.oc_clip_grad_norm_workspace(None, 3, ctypes.byref(nb)) == -1
+    assert L.oc_clip_grad_norm_workspace((I64 * 1)(5), 1, None) == -1
+    assert L.oc_clip_grad_norm_workspace((I64 * 1)(5), 1, ctypes.byref(nb)) == 0 and nb.value >= 8
+
+
+def test_binding_refuses_tensors_it_cannot_take():
+    """The binding's own checks, before the library is called."""
+    from paper_1611_05009_amd import octnet as oc
+    q = torch.zeros(4, 2, 16)
+    with pytest.raises(oc.OctNetError):
+        oc.attention(q, q, q)                                   # not on the GPU
+    with pytest.raises(oc.OctNetError):
+        oc.attention(q, q[:, :, :8], q[:, :, :8])               # head sizes differ
+    with pytest.raises(oc.OctNetError):
+        oc.attention(q, q.half(), q.half())                     # types differ
+    with pytest.raises(oc.OctNetError):
+        oc.attention(q, q, q, q_offsets=torch.zeros(2, dtype=torch.int64))
+    with pytest.raises(oc.OctNetError):
+        oc.rms_norm(torch.zeros(4, 8), torch.ones(8))
+    with pytest.raises(oc.OctNetError):
+        oc.rms_norm(torch.zeros(4, 8), torch.ones(7))
+    with pytest.raises(oc.OctNetError):
+        oc.rms_norm(torch.zeros(8), torch.ones(8))
+    with pytest.raises(oc.OctNetError):
+        oc.label_logprobs(torch.zeros(4, 8), torch.zeros(4, dtype=torch.int64))
+    with pytest.raises(oc.OctNetError):
+        oc.label_logprobs(torch.zeros(4, 8), torch.zeros(3, dtype=torch.int32))
+    with pytest.raises(oc.OctNetError):
+        oc.clip_grad_norm([torch.zeros(4)], 1.0)
