@@ -514,7 +514,8 @@ int oc_points_vote(const int32_t* rows, int64_t n_pts, const int32_t* labels, in
  * Where the rows are too few to fill the device the keys are split and
  * the parts joined, in a fixed order: results do not vary from run to run.
  */
-int oc_attention_workspace(int64_t n_q, int64_t n_k, int n_seq, int heads, int kv_heads, int dim, size_t* bytes);
+int oc_attention_workspace(int64_t n_q, int64_t n_k, int n_seq, int heads, int kv_heads, int dim, int dtype,
+                           size_t* bytes);
 int oc_attention(const void* q, int64_t q_row, int64_t q_head, const void* k, int64_t k_row, int64_t k_head,
                  const void* v, int64_t v_row, int64_t v_head, const int64_t* q_off, const int64_t* k_off,
                  const int64_t* k_len, int n_seq, int64_t n_q, int64_t n_k, int heads, int kv_heads, int dim,
@@ -527,7 +528,7 @@ int oc_attention(const void* q, int64_t q_row, int64_t q_head, const void* k, in
  * the sums over its group, added up in a fixed order.  Keys must fill their
  * ranges (no k_len). */
 int oc_attention_backward_workspace(int64_t n_q, int64_t n_k, int n_seq, int heads, int kv_heads, int dim,
-                                    size_t* bytes);
+                                    int dtype, size_t* bytes);
 int oc_attention_backward(const void* q, int64_t q_row, int64_t q_head, const void* k, int64_t k_row,
                           int64_t k_head, const void* v, int64_t v_row, int64_t v_head, const void* out,
                           const float* lse, const void* dout, const int64_t* q_off, const int64_t* k_off,

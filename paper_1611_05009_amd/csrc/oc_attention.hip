@@ -152,6 +152,13 @@ struct Tile {
     return row * (kChunks * 16) + row / kGroup * kPad + at(r, chunk);
   }
 
+  static __device__ __forceinline__ float get(const char* t, int r, int c) {
+    return (float)*(const T*)(t + at(r, c / kPer) + c % kPer * (int)sizeof(T));
+  }
+  static __device__ __forceinline__ void clear(char* t, int r, int c) {
+    *(T*)(t + at(r, c / kPer) + c % kPer * (int)sizeof(T)) = (T)0.f;
+  }
+
   // This lane's part of its addresses: those of a row-wise read start at
   // row_at + row_x, those of a column read at col_at + col_x, and the column
   // changes what the swizzle may change (kSwaps) by exclusive or.
@@ -471,14 +478,84 @@ struct Plan {
 };
 
 // ---------------------------------------------------------------------------
+// Infinities and NaN in masked places
+// ---------------------------------------------------------------------------
+//
+// A masked place enters a product as a factor of zero, and zero times an
+// infinity or NaN is NaN: a key that a row does not see could still reach it.
+// Only a causal mask hides rows that exist (past the end of a sequence the
+// tiles hold zeros), so only the steps on its edge are looked at: clean()
+// leaves zeros in the place of such elements before the products read the
+// tile, and where there were any, poison() brings them from global memory
+// straight to the accumulators that see them.
+
+__device__ __forceinline__ bool is_finite(float x) { return x - x == 0.f; }
+
+// The bits of a word that are the signs of its elements whose exponent is all
+// ones, and zeros in the place of those elements.
+template <class T>
+__device__ __forceinline__ uint32_t not_finite(uint32_t x) {
+  if constexpr (sizeof(T) == 4) return ((x & 0x7f800000u) + 0x00800000u) & 0x80000000u;
+  if constexpr (std::is_same<T, __bf16>::value) return ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+  return ((x & 0x7c007c00u) + 0x04000400u) & 0x80008000u;
+}
+template <class T>
+__device__ __forceinline__ uint32_t without(uint32_t x, uint32_t signs) {
+  return x & ~(sizeof(T) == 4 ? (uint32_t)((int32_t)signs >> 31) : (signs >> 15) * 0xffffu);
+}
+
+// By the whole workgroup, a barrier at its end; true if anything was found.
+template <class T, int D, int R, int NT>
+__device__ __forceinline__ bool clean(char* tile) {
+  using L = Tile<T, D, R>;
+  bool found = false;
+#pragma unroll 1
+  for (int n = (int)threadIdx.x; n < R * L::kChunks; n += NT) {
+    u32x4* p = (u32x4*)(tile + n / 64 * (1024 + L::kPad) + n % 64 * 16);
+    u32x4 x = *p;
+    const uint32_t any = not_finite<T>(x[0]) | not_finite<T>(x[1]) | not_finite<T>(x[2]) | not_finite<T>(x[3]);
+    if (any) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = without<T>(x[i], not_finite<T>(x[i]));
+      *p = x;
+      found = true;
+    }
+  }
+  return __syncthreads_or(found);
+}
+
+// Adds the infinite and NaN elements of rows j0 .. j1 - 1 (row_at(j): where
+// they lie in global memory) that this lane's column `sees` to its accumulators.
+template <class T, int D, class P, class F>
+__device__ __forceinline__ void poison(f32x16* o, int j0, int j1, int dim, P row_at, F sees) {
+  const int h = lane() >> 5;
+#pragma unroll 1
+  for (int j = j0; j < j1; ++j) {
+    const T* row = row_at(j);
+    bool bad = false;
+    for (int d = lane(); d < dim; d += 64) bad |= !is_finite((float)row[d]);
+    if (!__any(bad)) continue;
+    const bool see = sees(j);
+#pragma unroll
+    for (int n = 0; n < D / 32; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int d = 32 * n + 8 * (i / 4) + 4 * h + i % 4;
+        const float x = d < dim ? (float)row[d] : 0.f;
+        o[n][i] += see && !is_finite(x) ? x : 0.f;
+      }
+  }
+}
+
+// ---------------------------------------------------------------------------
 // Forward
 // ---------------------------------------------------------------------------
 
-// NW waves of MT x 32 packed rows each, BN keys per step, two LDS buffers.
-template <class T, int D, int MT, int NW, int BN>
+// NW waves of 32 packed rows each, BN keys per step, two LDS buffers.
+template <class T, int D, int NW, int BN>
 __global__ __launch_bounds__(NW * 64, 2) void k_attention(AttnArgs a) {
   using L = Tile<T, D, BN>;
-  constexpr int NT = NW * 64, BM = NW * MT * 32;
+  constexpr int NT = NW * 64, BM = NW * 32;
   __shared__ __attribute__((aligned(16))) char lds[2][2][L::kBytes];
 
   const Item item(a);
@@ -505,33 +582,16 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention(AttnArgs a) {
   const T* k = (const T*)a.k + e.k0 * a.k_row + (int64_t)kvh * a.k_head;
   const T* v = (const T*)a.v + e.k0 * a.v_row + (int64_t)kvh * a.v_head;
 
-  frag_t<T> qf[MT][D / 16];
-  int seen[MT], seen_min[MT], seen_max = 0;
+  const int w0 = r0 + w * 32, r = w0 + l32;  // the wave's first row, and the lane's
+  const int rr = r < rows ? r : rows - 1;
+  const int seen = seen_keys(a, e, rr);
+  const int seen_min = __builtin_amdgcn_readfirstlane(seen_keys(a, e, w0 < rows ? w0 : rows - 1));
+  const int seen_max =
+      __builtin_amdgcn_readfirstlane(w0 < rows ? seen_keys(a, e, w0 + 31 < rows ? w0 + 31 : rows - 1) : 0);
+  const T* qp = q + row_offset(a, rr, a.q_row, a.q_head);
+  frag_t<T> qf[D / 16];
 #pragma unroll
-  for (int m = 0; m < MT; ++m) {
-    const int w0 = r0 + (w * MT + m) * 32;  // first row of the 32
-    const int r = w0 + l32;
-    const int rr = r < rows ? r : rows - 1;
-    seen[m] = seen_keys(a, e, rr);
-    seen_min[m] = __builtin_amdgcn_readfirstlane(seen_keys(a, e, w0 < rows ? w0 : rows - 1));
-    const T* qp = q + row_offset(a, rr, a.q_row, a.q_head);
-#pragma unroll
-    for (int i = 0; i < D / 16; ++i) qf[m][i] = global_frag<T>(qp, true, 16 * i, a.dim);
-    const int e1 = w0 + 31 < rows ? w0 + 31 : rows - 1;
-    const int mx = w0 < rows ? seen_keys(a, e, e1) : 0;
-    seen_max = mx > seen_max ? mx : seen_max;
-  }
-  seen_max = __builtin_amdgcn_readfirstlane(seen_max);
-
-  f32x16 o[MT][D / 32];
-  float mx[MT], sum[MT];
-#pragma unroll
-  for (int m = 0; m < MT; ++m) {
-    mx[m] = -OC_INF;
-    sum[m] = 0.f;
-#pragma unroll
-    for (int d = 0; d < D / 32; ++d) o[m][d] = zero16();
-  }
+  for (int i = 0; i < D / 16; ++i) qf[i] = global_frag<T>(qp, true, 16 * i, a.dim);
   const float c = a.scale * kLog2e;
 
   const Stage<T, D, BN, NT> stage;
@@ -540,104 +600,101 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention(AttnArgs a) {
     stage.copy(lds[b][0], k + j * a.k_row, a.k_row, e.lk - (int)j, a.dim);
     stage.copy(lds[b][1], v + j * a.v_row, a.v_row, e.lk - (int)j, a.dim);
   };
+  f32x16 o[D / 32];
+  float mx = -OC_INF, sum = 0.f;
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d) o[d] = zero16();
+  // First step that hides a key from a row of the workgroup.
+  const int edge = a.causal ? seen_keys(a, e, r0) / BN : t1;
+  bool found = false;
   if (t0 < t1) load(t0, 0);
   wait_copies();
   typename L::Lanes ln;
   for (int t = t0; t < t1; ++t) {
     ln.renew();
     const char* kt = lds[(t - t0) & 1][0];
-    const char* vt = lds[(t - t0) & 1][1];
+    char* vt = lds[(t - t0) & 1][1];
     if (t + 1 < t1) load(t + 1, (t + 1 - t0) & 1);
+    if (t >= edge) found |= clean<T, D, BN, NT>(vt);
     if (t * BN < seen_max) {
-      f32x16 x[MT][BN / 32];
+      f32x16 x[BN / 32];
 #pragma unroll
       for (int n = 0; n < BN / 32; ++n) {
+        x[n] = zero16();
 #pragma unroll
-        for (int m = 0; m < MT; ++m) x[m][n] = zero16();
-#pragma unroll
-        for (int i = 0; i < D / 16; ++i) {
-          const frag_t<T> kf = L::rows(kt, ln, 32 * n, 16 * i);
-#pragma unroll
-          for (int m = 0; m < MT; ++m) x[m][n] = mma(kf, qf[m][i], x[m][n]);
-        }
+        for (int i = 0; i < D / 16; ++i) x[n] = mma(L::rows(kt, ln, 32 * n, 16 * i), qf[i], x[n]);
       }
       // 907 to 924 TFLOP/s at head size 128; smaller ones gain nothing.
       if constexpr (sizeof(T) == 2 && D > 64) pace<4, BN / 32 * (D / 16) - 4, 1, 4>();
-#pragma unroll
-      for (int m = 0; m < MT; ++m) {
-        if ((t + 1) * BN > seen_min[m]) {
-#pragma unroll
-          for (int n = 0; n < BN / 32; ++n)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const int key = t * BN + 32 * n + 8 * (i / 4) + 4 * h + i % 4;
-              x[m][n][i] = key >= seen[m] ? -OC_INF : x[m][n][i];
-            }
-        }
-        float top = x[m][0][0];
-#pragma unroll
-        for (int n = 0; n < BN / 32; ++n)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) top = fmaxf(top, x[m][n][i]);
-        top = half_max(top);
-        // The running maximum may lag the true one by up to 8 in base 2: the
-        // sums stay exact ratios, and most steps need no rescaling.
-        if (__any((top - mx[m]) * c > 8.f)) {
-          const float now = fmaxf(mx[m], top);
-          const float f = now == -OC_INF ? 1.f : __builtin_amdgcn_exp2f((mx[m] - now) * c);
-          mx[m] = now;
-          sum[m] *= f;
-#pragma unroll
-          for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[m][d][i] *= f;
-        }
-        const float off = mx[m] == -OC_INF ? 0.f : -mx[m] * c;
+      if ((t + 1) * BN > seen_min) {
 #pragma unroll
         for (int n = 0; n < BN / 32; ++n)
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            x[m][n][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[m][n][i], c, off));
-            sum[m] += x[m][n][i];
+            const int key = t * BN + 32 * n + 8 * (i / 4) + 4 * h + i % 4;
+            x[n][i] = key >= seen ? -OC_INF : x[n][i];
           }
       }
+      float top = x[0][0];
+#pragma unroll
+      for (int n = 0; n < BN / 32; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, x[n][i]);
+      top = half_max(top);
+      // The running maximum may lag the true one by up to 8 in base 2: the
+      // sums stay exact ratios, and most steps need no rescaling.
+      if (__any((top - mx) * c > 8.f)) {
+        const float now = fmaxf(mx, top);
+        const float f = now == -OC_INF ? 1.f : __builtin_amdgcn_exp2f((mx - now) * c);
+        mx = now;
+        sum *= f;
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[d][i] *= f;
+      }
+      const float off = mx == -OC_INF ? 0.f : -mx * c;
+#pragma unroll
+      for (int n = 0; n < BN / 32; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          x[n][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[n][i], c, off));
+          sum += x[n][i];
+        }
+      // Probabilities are rounded to the type for the product, as its operand;
+      // their sum is of the unrounded ones.
 #pragma unroll
       for (int n = 0; n < BN / 32; ++n)
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          frag_t<T> pf[MT];
+          const frag_t<T> pf = to_frag<T>(x[n], 8 * j);
 #pragma unroll
-          for (int m = 0; m < MT; ++m) pf[m] = to_frag<T>(x[m][n], 8 * j);
-#pragma unroll
-          for (int d = 0; d < D / 32; ++d) {
-            const frag_t<T> vf = L::cols(vt, ln, 32 * n + 16 * j, 32 * d);
-#pragma unroll
-            for (int m = 0; m < MT; ++m) o[m][d] = mma(vf, pf[m], o[m][d]);
-          }
+          for (int d = 0; d < D / 32; ++d) o[d] = mma(L::cols(vt, ln, 32 * n + 16 * j, 32 * d), pf, o[d]);
         }
     }
     wait_copies();
   }
+  if (found) {
+    const int end = t1 * BN < e.lk ? t1 * BN : e.lk;
+    poison<T, D>(o, (edge > t0 ? edge : t0) * BN, end, a.dim, [&](int j) { return v + j * a.v_row; },
+                 [&](int j) { return j < seen; });
+  }
 
+  if (r >= rows) return;
+  const float total = half_sum(sum);
+  const float f = total > 0.f || total != total ? 1.f / total : 0.f;
+  const float lse = total == 0.f ? -OC_INF : (mx * c + __builtin_amdgcn_logf(total)) * kLn2;
+  const int qi = by_group(a, r);
+  const int64_t at = (e.q0 + qi) * a.heads + (int64_t)kvh * a.group + (r - qi * a.group);
+  if (a.n_split > 1) {
+    const int64_t part = (int64_t)item.part * a.n_q * a.heads + at;
+    if (h == 0) a.part_lse[part] = lse;
 #pragma unroll
-  for (int m = 0; m < MT; ++m) {
-    const int r = r0 + (w * MT + m) * 32 + l32;
-    if (r >= rows) continue;
-    const float total = half_sum(sum[m]);
-    const float f = total > 0.f || total != total ? 1.f / total : 0.f;
-    const float lse = total == 0.f ? -OC_INF : (mx[m] * c + __builtin_amdgcn_logf(total)) * kLn2;
-    const int qi = by_group(a, r);
-    const int64_t at = (e.q0 + qi) * a.heads + (int64_t)kvh * a.group + (r - qi * a.group);
-    if (a.n_split > 1) {
-      const int64_t part = (int64_t)item.part * a.n_q * a.heads + at;
-      if (h == 0) a.part_lse[part] = lse;
+    for (int d = 0; d < D / 32; ++d) store_col<float>(a.part + part * a.dim, o[d], 32 * d, a.dim, f);
+  } else {
+    if (h == 0) a.lse[at] = lse;
 #pragma unroll
-      for (int d = 0; d < D / 32; ++d) store_col<float>(a.part + part * a.dim, o[m][d], 32 * d, a.dim, f);
-    } else {
-      if (h == 0) a.lse[at] = lse;
-#pragma unroll
-      for (int d = 0; d < D / 32; ++d) store_col<T>((T*)a.out + at * a.dim, o[m][d], 32 * d, a.dim, f);
-    }
+    for (int d = 0; d < D / 32; ++d) store_col<T>((T*)a.out + at * a.dim, o[d], 32 * d, a.dim, f);
   }
 }
 
@@ -737,8 +794,6 @@ __global__ __launch_bounds__(NW * 64, (Plan<T, D>::kDqWaves)) void k_attention_d
     a.lse2[at] = lse2;
   }
   f32x16 g[D / 32];
-#pragma unroll
-  for (int d = 0; d < D / 32; ++d) g[d] = zero16();
   const float c = a.scale * kLog2e;
 
   const Stage<T, D, BN, NT> stage;
@@ -747,14 +802,19 @@ __global__ __launch_bounds__(NW * 64, (Plan<T, D>::kDqWaves)) void k_attention_d
     stage.copy(lds[b][0], k + j * a.k_row, a.k_row, e.lk - (int)j, a.dim);
     stage.copy(lds[b][1], v + j * a.v_row, a.v_row, e.lk - (int)j, a.dim);
   };
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d) g[d] = zero16();
+  const int edge = a.causal ? seen_keys(a, e, r0) / BN : t1;
+  bool found = false;
   if (t0 < t1) load(t0, 0);
   wait_copies();
   typename L::Lanes ln;
   for (int t = t0; t < t1; ++t) {
     ln.renew();
-    const char* kt = lds[(t - t0) & 1][0];
+    char* kt = lds[(t - t0) & 1][0];
     const char* vt = lds[(t - t0) & 1][1];
     if (t + 1 < t1) load(t + 1, (t + 1 - t0) & 1);
+    if (t >= edge) found |= clean<T, D, BN, NT>(kt);
     if (t * BN < seen_max) {
 #pragma unroll
       for (int n = 0; n < BN / 32; ++n) {
@@ -782,6 +842,11 @@ __global__ __launch_bounds__(NW * 64, (Plan<T, D>::kDqWaves)) void k_attention_d
       }
     }
     wait_copies();
+  }
+  if (found) {
+    const int end = t1 * BN < e.lk ? t1 * BN : e.lk;
+    poison<T, D>(g, (edge > t0 ? edge : t0) * BN, end, a.dim, [&](int j) { return k + j * a.k_row; },
+                 [&](int j) { return j < seen; });
   }
   if (r < rows) {
 #pragma unroll
@@ -839,8 +904,6 @@ __global__ __launch_bounds__(NW * 64, (Plan<T, D>::kDkvWaves)) void k_attention_
     if constexpr (!kLds) vf[i] = global_frag<T>(v + (int64_t)(valid ? key : 0) * a.v_row, valid, 16 * i, a.dim);
   }
   f32x16 gk[D / 32], gv[D / 32];
-#pragma unroll
-  for (int d = 0; d < D / 32; ++d) gk[d] = gv[d] = zero16();
   const float c = a.scale * kLog2e;
   constexpr float kUp = (float)(1 << Frag<T>::kShift), kDown = 1.f / kUp;
 
@@ -856,7 +919,7 @@ __global__ __launch_bounds__(NW * 64, (Plan<T, D>::kDkvWaves)) void k_attention_
       const int r = t * BQ + (int)threadIdx.x;
       const int64_t at = at0 + row_offset(a, r < rows ? r : rows - 1, a.heads, 1);
       ss = r < rows ? a.lse2[at] - (float)Frag<T>::kShift : OC_INF;
-      sd = a.delta[at] * kDown;
+      sd = r < rows ? a.delta[at] * kDown : 0.f;
     }
   };
   const auto store = [&](int b) {
@@ -866,6 +929,11 @@ __global__ __launch_bounds__(NW * 64, (Plan<T, D>::kDkvWaves)) void k_attention_
     }
   };
   if constexpr (kLds) Stage<T, D, BK, NT>().copy(vt, v + j0 * a.v_row, a.v_row, e.lk - j0, a.dim);
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d) gk[d] = gv[d] = zero16();
+  // Rows before this one do not see all keys of the workgroup.
+  const int64_t edge = a.causal ? (int64_t)(j0 + BK - 1 - (e.lk - e.lq)) * a.group : 0;
+  bool found = false;
   if (t0 < t1) {
     load(t0, 0);
     store(0);
@@ -877,9 +945,13 @@ __global__ __launch_bounds__(NW * 64, (Plan<T, D>::kDkvWaves)) void k_attention_
     ln.renew();
     lk.renew();
     const int b = (t - t0) & 1;
-    const char* qt = lds[b][0];
-    const char* dt = lds[b][1];
+    char* qt = lds[b][0];
+    char* dt = lds[b][1];
     if (t + 1 < t1) load(t + 1, (t + 1 - t0) & 1);
+    if ((int64_t)t * BQ < edge) {
+      found |= clean<T, D, BQ, NT>(qt);
+      found |= clean<T, D, BQ, NT>(dt);
+    }
 #pragma unroll
     for (int n = 0; n < BQ / 32; ++n) {
       f32x16 x = zero16(), y = zero16();
@@ -932,6 +1004,12 @@ __global__ __launch_bounds__(NW * 64, (Plan<T, D>::kDkvWaves)) void k_attention_
     }
     if (t + 1 < t1) store((t + 1 - t0) & 1);
     wait_copies();
+  }
+  if (found) {
+    const int end = t1 * BQ < rows ? t1 * BQ : rows;
+    const auto sees = [&](int j) { return key < seen_keys(a, e, j); };
+    poison<T, D>(gk, t0 * BQ, end, a.dim, [&](int j) { return q + row_offset(a, j, a.q_row, a.q_head); }, sees);
+    poison<T, D>(gv, t0 * BQ, end, a.dim, [&](int j) { return dout + row_offset(a, j, a.heads, 1) * a.dim; }, sees);
   }
   if (valid) {
     const int64_t at = ((e.k0 + key) * a.kv_heads + kvh) * a.dim, n = a.n_k * a.kv_heads * a.dim;
@@ -995,31 +1073,40 @@ void attention_set_group(AttnArgs* a) {
 constexpr int kWaves = 4, kTile = 32 * kWaves;
 
 // Parts in which each tile's steps are taken so that there are `wanted`
-// workgroups, each with two steps at least on average.
-static int parts_of(int64_t workgroups, int64_t wanted, int64_t steps) {
+// workgroups, each with `least` steps at least on average.
+static int parts_of(int64_t workgroups, int64_t wanted, int64_t steps, int64_t least) {
   int64_t n = (wanted + workgroups - 1) / workgroups;
-  if (n > steps / 2) n = steps / 2;
+  if (n > steps / least) n = steps / least;
   if (n > 64) n = 64;
   return n < 1 ? 1 : (int)n;
 }
 
-// The device holds two workgroups per CU.  Sequences whose rows fit one wave
-// (single tokens) only stream their keys: many short parts keep the loads
-// going and even out the lengths (32 sequences of up to 8192 keys: 302 us in
-// one part).
-int attention_splits(int64_t n_q, int64_t n_k, int n_seq, int heads, int kv_heads) {
-  const int64_t workgroups = slots_of(n_q * (heads / kv_heads), kTile, n_seq) * kv_heads;
-  const int64_t steps = n_k / n_seq / 64;
-  if (n_q * (heads / kv_heads) <= 32 * (int64_t)n_seq) return parts_of(workgroups, 2048, steps);
-  return workgroups > 256 ? 1 : parts_of(workgroups, 512, steps);
+// The device holds two workgroups per CU.  Parts cost a write and a read of
+// float rows each, so in 16 bits only grids under half of the device are split;
+// 32-bit steps take 16 times as long and are worth it up to all of it (8192 rows
+// causal, 4 heads of 32: 316 us in one part, 186 in four).  Single steps are not
+// (937 rows, 4 heads of 64 over 2, with gradients: 97 us, in single steps 122).
+// Sequences whose rows fit one wave (single tokens) only
+// stream their keys: many short parts keep the loads going and even out the
+// lengths (32 sequences of up to 8192 keys: 302 us in one part, 135 in eight).
+static int row_parts(int64_t workgroups, int64_t steps, int dtype) {
+  if (dtype == kF32) return workgroups > 512 ? 1 : parts_of(workgroups, 1024, steps, 2);
+  return workgroups > 256 ? 1 : parts_of(workgroups, 512, steps, 2);
 }
 
-AttnParts attention_back_parts(int64_t n_q, int64_t n_k, int n_seq, int heads, int kv_heads, int dim) {
+int attention_splits(int64_t n_q, int64_t n_k, int n_seq, int heads, int kv_heads, int dtype) {
+  const int64_t rows = n_q * (heads / kv_heads), workgroups = slots_of(rows, kTile, n_seq) * kv_heads;
+  const int64_t steps = n_k / n_seq / 64;
+  return rows <= 32 * (int64_t)n_seq ? parts_of(workgroups, 2048, steps, 2) : row_parts(workgroups, steps, dtype);
+}
+
+AttnParts attention_back_parts(int64_t n_q, int64_t n_k, int n_seq, int heads, int kv_heads, int dim, int dtype) {
   AttnParts p;
   const int64_t rows = n_q * (heads / kv_heads);
-  const int64_t wq = slots_of(rows, kTile, n_seq) * kv_heads, wk = slots_of(n_k, kTile, n_seq) * kv_heads;
-  p.dq = wq > 256 ? 1 : parts_of(wq, 512, n_k / n_seq / 64);
-  p.dkv = parts_of(wk, 1024, rows / n_seq / 64);
+  p.dq = row_parts(slots_of(rows, kTile, n_seq) * kv_heads, n_k / n_seq / 64, dtype);
+  // Causal tiles differ by far in their work; twice as many workgroups as the
+  // device holds even it out (432 TFLOP/s with one part, 749 with two).
+  p.dkv = parts_of(slots_of(n_k, kTile, n_seq) * kv_heads, 1024, rows / n_seq / 64, 2);
   const int64_t a = p.dq > 1 ? p.dq * n_q * heads : 0, b = p.dkv > 1 ? 2 * p.dkv * n_k * kv_heads : 0;
   p.bytes = (size_t)(a > b ? a : b) * dim * sizeof(float);
   return p;
@@ -1031,7 +1118,7 @@ hipError_t launch_attention(const AttnArgs& a, int dtype, hipStream_t s) {
     using T = decltype(t);
     const hipError_t err = by_dim(a.dim, [&](auto d) {
       constexpr int D = decltype(d)::value;
-      k_attention<T, D, 1, kWaves, Plan<T, D>::kKeys>
+      k_attention<T, D, kWaves, Plan<T, D>::kKeys>
           <<<(unsigned)(workgroups * a.n_split), kWaves * 64, 0, s>>>(a);
       return hipGetLastError();
     });
@@ -1052,7 +1139,7 @@ static hipError_t sum_parts(const float* part, int64_t n, int parts, void* out0,
 }
 
 hipError_t launch_attention_backward(AttnArgs a, int dtype, hipStream_t s) {
-  const AttnParts parts = attention_back_parts(a.n_q, a.n_k, a.n_seq, a.heads, a.kv_heads, a.dim);
+  const AttnParts parts = attention_back_parts(a.n_q, a.n_k, a.n_seq, a.heads, a.kv_heads, a.dim, dtype);
   return by_type(dtype, [&](auto t) {
     using T = decltype(t);
     hipError_t err = hipSuccess;

@@ -39,23 +39,22 @@ __device__ __forceinline__ float exp2n(float z) { return __builtin_amdgcn_exp2f(
 __device__ __forceinline__ float bounded(float z) { return fmaxf(z, -1e4f); }
 
 // Running maximum m, and with z = log2(e) (x - m): sums of 2^z and of z 2^z.
-// base is log2(e) m as rounded: what it is off the product is common to all
-// terms and to the result's first term.
+// The difference comes first: multiples of the type's lowest value, which some
+// masks are made of, would overflow.
 struct Stat {
-  float m = -OC_INF, base = 0.f, s = 0.f, t = 0.f;
+  float m = -OC_INF, s = 0.f, t = 0.f;
 
+  __device__ __forceinline__ float base() const { return m == -OC_INF ? 0.f : m; }
   __device__ __forceinline__ void rescale(float now) {
-    const float next = now == -OC_INF ? 0.f : now * kLog2e;
     if (now != m && m != -OC_INF) {
-      const float d = base - next, f = exp2n(d);
+      const float d = (m - now) * kLog2e, f = exp2n(d);
       t = f * (t + s * bounded(d));
       s *= f;
     }
     m = now;
-    base = next;
   }
   __device__ __forceinline__ void add(float x) {
-    const float z = __builtin_fmaf(x, kLog2e, -base), e = exp2n(z);
+    const float z = (x - base()) * kLog2e, e = exp2n(z);
     s += e;
     t += e * bounded(z);
   }
@@ -67,22 +66,21 @@ struct Stat {
     t += o.t;
   }
   __device__ __forceinline__ bool empty() const { return m == -OC_INF && s == 0.f; }  // every class ruled out
-  __device__ __forceinline__ float lse() const { return empty() ? -OC_INF : (base + log2f(s)) * kLn2; }
+  __device__ __forceinline__ float lse() const { return empty() ? -OC_INF : m + log2f(s) * kLn2; }
+  // x - lse, without the rounding of lse.
+  __device__ __forceinline__ float logp(float x) const { return (x - m) - log2f(s) * kLn2; }
   __device__ __forceinline__ float entropy() const {
     const float h = (log2f(s) - t / s) * kLn2;
     return empty() || h < 0.f ? 0.f : h;
-  }
-  __device__ __forceinline__ void set(float m_, float s_, float t_) {
-    rescale(m_);
-    s = s_;
-    t = t_;
   }
 };
 
 __device__ __forceinline__ Stat group_stat(Stat a, int width) {
   for (int i = width >> 1; i; i >>= 1) {
     Stat o;
-    o.set(__shfl_xor(a.m, i), __shfl_xor(a.s, i), __shfl_xor(a.t, i));
+    o.m = __shfl_xor(a.m, i);
+    o.s = __shfl_xor(a.s, i);
+    o.t = __shfl_xor(a.t, i);
     a.join(o);
   }
   return a;
@@ -103,10 +101,10 @@ __device__ __forceinline__ void group_best(float& v, int& i, int width) {
 }
 
 // What a row's statistics say of its label.
-__device__ __forceinline__ void write_row(const LabelArgs& a, int64_t row, const Stat& st, float lse, float mine) {
-  a.lse[row] = lse;
+__device__ __forceinline__ void write_row(const LabelArgs& a, int64_t row, const Stat& st, float mine) {
+  a.lse[row] = st.lse();
   const int label = a.labels[row];
-  a.logprob[row] = label < 0 || label >= a.classes ? 0.f : st.empty() ? -OC_INF : mine - lse;
+  a.logprob[row] = label < 0 || label >= a.classes ? 0.f : st.empty() ? -OC_INF : st.logp(mine);
   if (a.entropy) a.entropy[row] = st.entropy();
 }
 
@@ -116,9 +114,9 @@ __device__ __forceinline__ float label_logit(const LabelArgs& a, int64_t row) {
   return label < 0 || label >= a.classes ? 0.f : (float)((const T*)a.logits)[row * a.classes + label];
 }
 
-__device__ __forceinline__ void write_top(const LabelArgs& a, int64_t row, int k, float v, int i, float lse) {
+__device__ __forceinline__ void write_top(const LabelArgs& a, int64_t row, int k, float v, int i, const Stat& st) {
   a.top_label[row * a.top + k] = i == kNone ? -1 : i;
-  a.top_logprob[row * a.top + k] = i == kNone ? __builtin_nanf("") : v == -OC_INF ? v : v - lse;
+  a.top_logprob[row * a.top + k] = i == kNone ? __builtin_nanf("") : v == -OC_INF ? v : st.logp(v);
 }
 
 // ---------------------------------------------------------------------------
@@ -185,8 +183,7 @@ __global__ __launch_bounds__(256) void k_labels_held(LabelArgs a) {
       for (int i = 0; i < 8; ++i) st.add(r.x[v][i]);
     st.s = group_sum(st.s, a.lanes);
     st.t = group_sum(st.t, a.lanes);
-    const float lse = st.lse();
-    if (r.t == 0) write_row(a, row, st, lse, label_logit<T>(a, row));
+    if (r.t == 0) write_row(a, row, st, label_logit<T>(a, row));
     // The best of what comes after the last one found.
     float last = OC_INF;
     int last_i = -1;
@@ -205,7 +202,7 @@ __global__ __launch_bounds__(256) void k_labels_held(LabelArgs a) {
           }
         }
       group_best(best, best_i, a.lanes);
-      if (r.t == 0) write_top(a, row, k, best, best_i, lse);
+      if (r.t == 0) write_top(a, row, k, best, best_i, st);
       last = best;
       last_i = best_i;
     }
@@ -392,17 +389,17 @@ __device__ __forceinline__ int head_of(const T* p, int n) {
 // the first of the others fill up, in order.
 template <class T>
 __device__ __forceinline__ void finish_top(const LabelArgs& a, int64_t row, const float* v, const int* i, int count,
-                                           float lse) {
-  if (lane() < count) write_top(a, row, lane(), v[lane()], i[lane()], lse);
+                                           const Stat& st) {
+  if (lane() < count) write_top(a, row, lane(), v[lane()], i[lane()], st);
   const T* x = (const T*)a.logits + row * a.classes;
   for (int64_t j = 0; count < a.top && j < a.classes; j += 64) {
     const bool hit = j + lane() < a.classes && (float)x[j + lane()] == -OC_INF;
     const uint64_t all = __ballot(hit);
     const int at = count + __builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, 0));
-    if (hit && at < a.top) write_top(a, row, at, -OC_INF, (int)(j + lane()), lse);
+    if (hit && at < a.top) write_top(a, row, at, -OC_INF, (int)(j + lane()), st);
     count += __popcll(all);
   }
-  if (lane() >= count && lane() < a.top) write_top(a, row, lane(), 0.f, kNone, lse);
+  if (lane() >= count && lane() < a.top) write_top(a, row, lane(), 0.f, kNone, st);
 }
 
 // One workgroup per row (blockIdx.x) and part of it (blockIdx.y).  Writes the
@@ -483,7 +480,9 @@ __global__ __launch_bounds__(256) void k_labels_streamed(LabelArgs a) {
   if (w) return;
   for (int i = 1; i < 4; ++i) {
     Stat o;
-    o.set(stats[0][i], stats[1][i], stats[2][i]);
+    o.m = stats[0][i];
+    o.s = stats[1][i];
+    o.t = stats[2][i];
     st.join(o);
   }
   if constexpr (TOP) {
@@ -507,9 +506,8 @@ __global__ __launch_bounds__(256) void k_labels_streamed(LabelArgs a) {
     }
     return;
   }
-  const float lse = st.lse();
-  if (lane() == 0) write_row(a, row, st, lse, label_logit<T>(a, row));
-  if constexpr (TOP) finish_top<T>(a, row, list.v, list.i, list.count, lse);
+  if (lane() == 0) write_row(a, row, st, label_logit<T>(a, row));
+  if constexpr (TOP) finish_top<T>(a, row, list.v, list.i, list.count, st);
 }
 
 // Joins the parts of a row: one wave per row.
@@ -522,12 +520,13 @@ __global__ __launch_bounds__(64) void k_labels_join(LabelArgs a) {
   for (int p = lane(); p < a.parts; p += 64) {
     Stat o;
     const float* q = a.part_stat + 3 * (row * a.parts + p);
-    o.set(q[0], q[1], q[2]);
+    o.m = q[0];
+    o.s = q[1];
+    o.t = q[2];
     st.join(o);
   }
   st = group_stat(st, 64);
-  const float lse = st.lse();
-  if (lane() == 0) write_row(a, row, st, lse, label_logit<T>(a, row));
+  if (lane() == 0) write_row(a, row, st, label_logit<T>(a, row));
   if constexpr (TOP) {
     List list{vals, idxs, 0, 0, -OC_INF};
     const int n = a.parts * a.top;
@@ -540,7 +539,7 @@ __global__ __launch_bounds__(64) void k_labels_join(LabelArgs a) {
       list.push(i != kNone, v, i);
     }
     list.shrink(a.top);
-    finish_top<T>(a, row, list.v, list.i, list.count, lse);
+    finish_top<T>(a, row, list.v, list.i, list.count, st);
   }
 }
 

@@ -9,7 +9,9 @@ Tensors: trees int32 [n_trees, 4] (the uint32 bit words), prefix int64
 """
 from __future__ import annotations
 
+import array
 import ctypes
+import functools
 import os
 from dataclasses import dataclass
 
@@ -77,10 +79,10 @@ SIGNATURES = {
     "oc_points_workspace": (_S, [_L, _I]),
     "oc_points_average": (_I, [_P, _L, _P, _I, _L, _P, _P, _S, _P]),
     "oc_points_vote": (_I, [_P, _L, _P, _I, _L, _P, _P, _S, _P]),
-    "oc_attention_workspace": (_I, [_L, _L, _I, _I, _I, _I, _P]),
+    "oc_attention_workspace": (_I, [_L, _L, _I, _I, _I, _I, _I, _P]),
     "oc_attention": (_I, [_P, _L, _L, _P, _L, _L, _P, _L, _L, _P, _P, _P, _I, _L, _L, _I, _I, _I, _I, _F, _I, _P,
                           _P, _P, _S, _P]),
-    "oc_attention_backward_workspace": (_I, [_L, _L, _I, _I, _I, _I, _P]),
+    "oc_attention_backward_workspace": (_I, [_L, _L, _I, _I, _I, _I, _I, _P]),
     "oc_attention_backward": (_I, [_P, _L, _L, _P, _L, _L, _P, _L, _L, _P, _P, _P, _P, _P, _I, _L, _L, _I, _I, _I,
                                    _I, _F, _I, _P, _P, _P, _P, _S, _P]),
     "oc_rms_norm": (_I, [_P, _I, _P, _I, _P, _L, _I, _F, _P, _P, _I, _P, _P]),
@@ -135,7 +137,9 @@ def _ptr(t):
 
 
 def _stream():
-    return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+    # torch.cuda.current_stream().cuda_stream without the Stream object, which
+    # takes longer to make than the smallest operators to run.
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def _dev():
@@ -525,6 +529,20 @@ def points_vote(g: Octree, rows: torch.Tensor, labels: torch.Tensor, n_labels: i
     return out
 
 
+@functools.lru_cache(maxsize=1024)
+def _workspace(name: str, *sizes) -> int:
+    """Bytes that the library's query `name` gives for these sizes."""
+    nb = ctypes.c_size_t(0)
+    _check(getattr(lib(), name)(*sizes, ctypes.byref(nb)), name)
+    return nb.value
+
+
+def _scratch(name: str, device, *sizes):
+    """A workspace for these sizes, or None where none is needed."""
+    nb = _workspace(name, *sizes)
+    return torch.empty(nb, dtype=torch.uint8, device=device) if nb else None
+
+
 def _type(t: torch.Tensor) -> int:
     if t.dtype not in _TYPES:
         raise OctNetError("expected float32, float16 or bfloat16, got %s" % t.dtype)
@@ -579,17 +597,14 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_offsets: torc
     (int64, see leaf_offsets; None: one sequence), of which k_lengths[s] hold
     keys (None: all).  causal: a row sees the keys up to its own place, the
     last query beside the last key.  scale: 1 / sqrt(dim) by default."""
-    dims = _attention_shapes(q, k, v, q_offsets, k_offsets)
-    n_seq, n_q, n_k, heads, kv_heads, dim = dims
+    n_seq, n_q, n_k, heads, kv_heads, dim = _attention_shapes(q, k, v, q_offsets, k_offsets)
     if out is None:
         out = torch.empty((n_q, heads, dim), dtype=q.dtype, device=q.device)
     elif tuple(out.shape) != (n_q, heads, dim) or out.dtype != q.dtype:
         raise OctNetError("out must be [n_q, heads, dim] of q's type")
     lse = torch.empty((n_q, heads), dtype=torch.float32, device=q.device)
-    nb = ctypes.c_size_t(0)
-    _check(lib().oc_attention_workspace(n_q, n_k, n_seq, heads, kv_heads, dim, ctypes.byref(nb)), "oc_attention_workspace")
-    if ws is None and nb.value:
-        ws = torch.empty(nb.value, dtype=torch.uint8, device=q.device)
+    if ws is None:
+        ws = _scratch("oc_attention_workspace", q.device, n_q, n_k, n_seq, heads, kv_heads, dim, _type(q))
     _check(lib().oc_attention(*_heads(q, "q"), *_heads(k, "k"), *_heads(v, "v"),
                               _offsets(q_offsets, n_seq + 1, "q_offsets"), _offsets(k_offsets, n_seq + 1, "k_offsets"),
                               _offsets(k_lengths, n_seq, "k_lengths"), n_seq, n_q, n_k, heads, kv_heads, dim, _type(q),
@@ -613,16 +628,14 @@ def attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: t
     dq = torch.empty((n_q, heads, dim), dtype=q.dtype, device=q.device)
     dk = torch.empty((n_k, kv_heads, dim), dtype=q.dtype, device=q.device)
     dv = torch.empty_like(dk)
-    nb = ctypes.c_size_t(0)
-    _check(lib().oc_attention_backward_workspace(n_q, n_k, n_seq, heads, kv_heads, dim, ctypes.byref(nb)),
-           "oc_attention_backward_workspace")
     if ws is None:
-        ws = torch.empty(nb.value, dtype=torch.uint8, device=q.device)
+        ws = _scratch("oc_attention_backward_workspace", q.device, n_q, n_k, n_seq, heads, kv_heads, dim, _type(q))
     _check(lib().oc_attention_backward(*_heads(q, "q"), *_heads(k, "k"), *_heads(v, "v"), _ptr(out), _ptr(lse), _ptr(dout),
                                        _offsets(q_offsets, n_seq + 1, "q_offsets"),
                                        _offsets(k_offsets, n_seq + 1, "k_offsets"), n_seq, n_q, n_k, heads, kv_heads, dim,
                                        _type(q), dim ** -0.5 if scale is None else scale, int(bool(causal)), _ptr(dq),
-                                       _ptr(dk), _ptr(dv), _ptr(ws), ws.numel(), _stream()), "oc_attention_backward")
+                                       _ptr(dk), _ptr(dv), _ptr(ws), 0 if ws is None else ws.numel(), _stream()),
+           "oc_attention_backward")
     return dq, dk, dv
 
 
@@ -683,9 +696,7 @@ def rms_norm_backward(h: torch.Tensor, weight: torch.Tensor, dy: torch.Tensor, d
     dx = torch.empty_like(h)
     dw = torch.empty(c, dtype=torch.float32, device=h.device) if need_weight else None
     if ws is None and need_weight:
-        nb = ctypes.c_size_t(0)
-        _check(lib().oc_rms_norm_backward_workspace(rows, c, ctypes.byref(nb)), "oc_rms_norm_backward_workspace")
-        ws = torch.empty(nb.value, dtype=torch.uint8, device=h.device)
+        ws = _scratch("oc_rms_norm_backward_workspace", h.device, rows, c)
     _check(lib().oc_rms_norm_backward(_ptr(h), _type(h), _norm_weight(weight, c), _ptr(dy), _type(dy), _ptr(dsum), rows, c,
                                       eps, _ptr(dx), _ptr(dw), _ptr(ws), 0 if ws is None else ws.numel(), _stream()),
            "oc_rms_norm_backward")
@@ -729,10 +740,8 @@ def label_logprobs(logits: torch.Tensor, labels: torch.Tensor, top: int = 0, ent
     if top:
         r.top_logprob = torch.empty((rows, top), dtype=torch.float32, device=dev)
         r.top_label = torch.empty((rows, top), dtype=torch.int32, device=dev)
-    nb = ctypes.c_size_t(0)
-    _check(lib().oc_label_logprobs_workspace(rows, classes, top, ctypes.byref(nb)), "oc_label_logprobs_workspace")
-    if ws is None and nb.value:
-        ws = torch.empty(nb.value, dtype=torch.uint8, device=dev)
+    if ws is None:
+        ws = _scratch("oc_label_logprobs_workspace", dev, rows, classes, top)
     _check(lib().oc_label_logprobs(_ptr(logits), _type(logits), _ptr(labels), rows, classes, top, _ptr(r.logprob),
                                    _ptr(r.lse), _ptr(r.entropy), _ptr(r.top_logprob), _ptr(r.top_label), _ptr(ws),
                                    0 if ws is None else ws.numel(), _stream()), "oc_label_logprobs")
@@ -760,34 +769,32 @@ def label_logprobs_backward(logits: torch.Tensor, labels: torch.Tensor, lse: tor
 
 
 def clip_grad_norm(grads, max_norm: float, out=None, ws: torch.Tensor | None = None) -> torch.Tensor:
-    """Scales the gradients (a sequence of GPU tensors, of any of the three
-    types) by min(1, max_norm / (norm + 1e-6)), in place or into `out`, and
+    """Scales the gradients (a list of GPU tensors, of any of the three types) by min(1, max_norm / (norm + 1e-6)), in place or into `out`, and
     returns their common norm, a float32 scalar on the GPU (nothing waits for
     it)."""
-    grads = list(grads)
-    n = len(grads)
+    src, count, kind = array.array("Q"), array.array("q"), array.array("i")
     for t in grads:
-        if not (t.is_cuda and t.is_contiguous()):
-            raise OctNetError("expected contiguous GPU tensors")
-        if t.dtype not in _TYPES:
-            raise OctNetError("expected float32, float16 or bfloat16, got %s" % t.dtype)
-    src = (_P * n)(*[t.data_ptr() for t in grads])
+        if t.dtype not in _TYPES or not t.is_cuda or not t.is_contiguous():
+            raise OctNetError("the gradients must be contiguous GPU tensors of float32, float16 or bfloat16")
+        src.append(t.data_ptr())
+        count.append(t.numel())
+        kind.append(_TYPES[t.dtype])
+    n = len(src)
     dst = src
     if out is not None:
-        out = list(out)
-        if len(out) != n:
+        dst = array.array("Q", [o.data_ptr() for o in out])
+        if len(dst) != n:
             raise OctNetError("out must match the gradients")
-        for t, o in zip(grads, out):
-            if o.dtype != t.dtype or o.shape != t.shape or not (o.is_cuda and o.is_contiguous()):
+        for o, c, k in zip(out, count, kind):
+            if o.numel() != c or _TYPES.get(o.dtype) != k or not o.is_cuda or not o.is_contiguous():
                 raise OctNetError("out must match the gradients")
-        dst = (_P * n)(*[o.data_ptr() for o in out])
-    counts = (_L * n)(*[t.numel() for t in grads])
-    types = (_I * n)(*[_TYPES[t.dtype] for t in grads])
-    norm = torch.empty((), dtype=torch.float32, device=grads[0].device if n else _dev())
+    norm = torch.empty((), dtype=torch.float32, device=_dev() if n == 0 else t.device)
+    counts, types = count.buffer_info()[0], kind.buffer_info()[0]
     if ws is None:
         nb = ctypes.c_size_t(0)
         _check(lib().oc_clip_grad_norm_workspace(counts, n, ctypes.byref(nb)), "oc_clip_grad_norm_workspace")
         ws = torch.empty(nb.value, dtype=torch.uint8, device=norm.device)
-    _check(lib().oc_clip_grad_norm(src, dst, counts, types, n, max_norm, _ptr(norm), _ptr(ws), ws.numel(), _stream()),
+    _check(lib().oc_clip_grad_norm(src.buffer_info()[0], dst.buffer_info()[0], counts, types, n, max_norm, _ptr(norm),
+                                   _ptr(ws), ws.numel(), _stream()),
            "oc_clip_grad_norm")
     return norm

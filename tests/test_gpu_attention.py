@@ -230,6 +230,47 @@ def test_outside_rows_do_not_matter():
         assert torch.equal(out[keep], want) and torch.equal(lse[keep], wl)
 
 
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("lengths,H,K,D", [([70, 300], 4, 1, 64), ([513], 2, 2, 128), ([1000, 3], 4, 4, 32)])
+def test_masked_infinities_and_nan(dtype, lengths, H, K, D):
+    """Infinite and NaN keys, values, queries and output gradients from one row
+    on: what only earlier rows and keys enter has the bits that it has
+    without them, and what they enter shows them."""
+    from paper_1611_05009_amd import octnet as oc
+    n, cut = sum(lengths), lengths[0] // 2 + 5
+    bad = torch.tensor([math.nan, math.inf, -math.inf, 1.0], device="cuda")
+    for what in ("v", "kv", "all"):
+        q, k, v, d = inputs(19, dtype, n, n, H, K, D)
+        off = offsets(lengths)
+        kw = dict(q_offsets=off, k_offsets=off, causal=True)
+        clean = oc.attention(q, k, v, **kw)
+        clean_g = oc.attention_backward(q, k, v, *clean, d, **kw)
+        for name, t in (("v", v), ("k", k), ("q", q), ("d", d)):
+            if what == "all" or name in what:
+                t[cut:lengths[0]] = bad[torch.arange(D, device="cuda") % 4].to(dtype)
+        out, lse = oc.attention(q, k, v, **kw)
+        rest = torch.cat([torch.arange(cut), torch.arange(lengths[0], n)]).cuda()
+        assert torch.equal(out[rest], clean[0][rest]) and torch.equal(lse[rest], clean[1][rest]), what
+        assert not torch.isfinite(out[cut:lengths[0]][..., :3]).any(), what
+        if what == "v":
+            continue
+        dq, dk, dv = oc.attention_backward(q, k, v, out, lse, d, **kw)
+        assert torch.equal(dq[rest], clean_g[0][rest]), what
+        own = torch.arange(lengths[0], n).cuda()
+        assert torch.equal(dk[own], clean_g[1][own]) and torch.equal(dv[own], clean_g[2][own]), what
+        assert not torch.isfinite(dk[:cut]).all() and not torch.isfinite(dv[:cut]).all(), what
+    # late keys that only late rows see keep their gradients where early rows are bad
+    q, k, v, d = inputs(19, dtype, n, n, H, K, D)
+    clean = oc.attention(q, k, v, **kw)
+    clean_g = oc.attention_backward(q, k, v, *clean, d, **kw)
+    q[:cut], d[:cut] = math.nan, math.inf
+    out, lse = oc.attention(q, k, v, **kw)
+    dq, dk, dv = oc.attention_backward(q, k, v, out, lse, d, **kw)
+    for got, want in zip((out, lse, dq, dk, dv), clean + clean_g):
+        assert torch.equal(got[cut:], want[cut:])
+    assert not torch.isfinite(dk[0]).any()
+
+
 def test_results_do_not_vary():
     from paper_1611_05009_amd import octnet as oc
     q, k, v, d = inputs(13, torch.bfloat16, 700, 700, 8, 2, 128)

@@ -277,6 +277,30 @@ def test_labels_few_left():
     assert b.entropy is None and float(b.logprob[1]) == 0.0 and float(b.logprob[2]) == 0.0
 
 
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("classes", [50, 3000])
+def test_labels_masked_by_the_lowest_value(dtype, classes):
+    """Masks of the type's lowest value instead of -infinity, alone and for a
+    whole row, and logits at the other end of the type."""
+    from paper_1611_05009_amd import octnet as oc
+    low, high = torch.finfo(dtype).min, torch.finfo(dtype).max
+    x = randn(8, 4, classes).to(dtype)
+    x[0, 10:] = low
+    x[1] = low
+    x[2, 5] = high
+    labels = torch.tensor([3, 7, 5, 0], dtype=torch.int32)
+    a = oc.label_logprobs(x.cuda(), labels.cuda(), top=3)
+    lp = torch.log_softmax(x.double(), 1)
+    want = lp.gather(1, labels.long()[:, None])[:, 0]
+    near(a.logprob, want, (classes + 64) * U32 * (1 + want.abs()), "logprob")
+    ent = torch.special.entr(lp.exp()).sum(1)
+    near(a.entropy, ent, (classes + 64) * U32 * (4 + 4 * ent), "entropy")
+    order = torch.sort(x.double(), dim=1, descending=True, stable=True).indices[:, :3]
+    assert torch.equal(a.top_label.cpu().long(), order)
+    d = oc.label_logprobs_backward(x.cuda(), labels.cuda(), a.lse, torch.ones(4, device="cuda"))
+    assert torch.isfinite(d).all() and not d[0, 10:].any()
+
+
 def test_labels_after_nan():
     """The first thousands of a long row are NaN, as are single places later:
     the alternatives come from the rest."""

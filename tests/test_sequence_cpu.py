@@ -51,15 +51,16 @@ def test_attention_refusals(L, back, rc, kw):
 def test_attention_workspaces(L):
     nb = ctypes.c_size_t(7)
     # many rows: no parts; single rows against long keys: parts
-    assert L.oc_attention_workspace(100000, 100000, 1, 8, 8, 64, ctypes.byref(nb)) == 0 and nb.value == 0
-    assert L.oc_attention_workspace(4, 40000, 4, 8, 1, 64, ctypes.byref(nb)) == 0 and nb.value > 0
+    assert L.oc_attention_workspace(100000, 100000, 1, 8, 8, 64, 2, ctypes.byref(nb)) == 0 and nb.value == 0
+    assert L.oc_attention_workspace(4, 40000, 4, 8, 1, 64, 2, ctypes.byref(nb)) == 0 and nb.value > 0
     assert attention(L, n_q=4, n_k=40000, heads=2, ws_bytes=100) == -3
     assert attention(L, n_q=4, n_k=40000, heads=2, ws=None) == -3
     assert attention(L, True, ws_bytes=16) == -3
     assert attention(L, True, dout=None) == -1 and attention(L, True, dk=None) == -1
-    assert L.oc_attention_workspace(4, 4, 1, 8, 3, 64, ctypes.byref(nb)) == -1
-    assert L.oc_attention_workspace(4, 4, 1, 8, 8, 64, None) == -1
-    assert L.oc_attention_backward_workspace(4, 4, 1, 8, 8, 7, ctypes.byref(nb)) == -1
+    assert L.oc_attention_workspace(4, 4, 1, 8, 3, 64, 2, ctypes.byref(nb)) == -1
+    assert L.oc_attention_workspace(4, 4, 1, 8, 8, 64, 2, None) == -1
+    assert L.oc_attention_backward_workspace(4, 4, 1, 8, 8, 7, 2, ctypes.byref(nb)) == -1
+    assert L.oc_attention_workspace(4, 4, 1, 8, 8, 64, 3, ctypes.byref(nb)) == -1
     # nothing to do
     assert attention(L, n_q=0, q=None, out=None, lse=None) == 0
 
