@@ -325,16 +325,18 @@ struct Place {
 
 // The x-th tile of sequences whose lengths only the device knows, from
 // rows / tile + n_seq numbers (an upper bound of all tiles; the rest find
-// none).  Up to 64 sequences, one per lane: tiles are counted by their number
+// none).  Up to 16 sequences, one per lane: tiles are counted by their number
 // in their sequence, greatest numbers first, so that the tiles with the most
 // work start first however lengths are mixed.  Sum over sequences of max(0, n
-// - l) tiles have number l or greater; l is found by bisection.  More
-// sequences: sequence s owns the numbers from first row / tile + s on, which
-// leaves room for its tiles whatever the lengths.
+// - l) tiles have number l or greater; l is found among 64 candidates at a
+// time.  More sequences even out by their count, and the search would take
+// longer than their tiles (64 sequences of 200 rows, 8 heads of 64 over 2: 28 us
+// with it, 20 without): sequence s owns the numbers from first row / tile + s
+// on, which leaves room for its tiles whatever the lengths; back: from the last.
 __device__ __forceinline__ Place place_of(const int64_t* off, int n_seq, int64_t rows, int mul, int tile, int64_t x,
-                                          int64_t numbers) {
+                                          int64_t numbers, bool back) {
   Place p{-1, 0, 0};
-  if (n_seq <= 64) {
+  if (n_seq <= 16) {
     int n = 0;
     if (!off) {
       n = lane() == 0 ? (int)((rows * mul + tile - 1) / tile) : 0;
@@ -342,8 +344,7 @@ __device__ __forceinline__ Place place_of(const int64_t* off, int n_seq, int64_t
       const int64_t a = bounded(off[lane()], 0, rows), b = bounded(off[lane() + 1], a, rows);
       n = (int)(((b - a) * mul + tile - 1) / tile);
     }
-    // Least l of which at most x tiles have greater numbers: 64 candidates at
-    // a time, one per lane.
+    // Least l of which at most x tiles have greater numbers.
     int hi = 0;  // one past the greatest number
     for (int s = 0; s < n_seq; ++s) {
       const int o = __builtin_amdgcn_readlane(n, s);
@@ -373,7 +374,7 @@ __device__ __forceinline__ Place place_of(const int64_t* off, int n_seq, int64_t
     p.n = __builtin_amdgcn_readlane(n, p.s);
     return p;
   }
-  x = numbers - 1 - x;
+  if (back) x = numbers - 1 - x;
   int lo = 0, count = n_seq;  // the answer lies in [lo, lo + count), 64 candidates per step
   while (count > 1) {
     const int step = (count + 63) / 64;
@@ -469,7 +470,7 @@ __device__ __forceinline__ void store_col(T* p, const f32x16& c, int d0, int dim
 template <class T, int D>
 struct Plan {
   static constexpr bool kWide = D > 64, kHalf = sizeof(T) == 2;
-  static constexpr int kKeys = kHalf && !kWide ? 128 : kHalf || !kWide ? 64 : 32;  // forward
+  static constexpr int kKeys = kHalf && D <= 32 ? 128 : kHalf || !kWide ? 64 : 32;  // forward
   static constexpr int kDqKeys = kHalf ? 64 : 32;
   static constexpr int kDqWaves = kHalf || !kWide ? 2 : 1;
   static constexpr int kDkvRows = kHalf && !kWide ? 64 : 32;
@@ -560,7 +561,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention(AttnArgs a) {
 
   const Item item(a);
   const int kvh = item.kvh;
-  const Place p = place_of(a.q_off, a.n_seq, a.n_q, a.group, BM, item.tile, item.tiles);
+  const Place p = place_of(a.q_off, a.n_seq, a.n_q, a.group, BM, item.tile, item.tiles, true);
   if (p.s < 0) return;
   const Seq e = seq_of(a, p.s);
   const int rows = e.lq * a.group;
@@ -734,9 +735,18 @@ __global__ __launch_bounds__(256) void k_attention_join(AttnArgs a) {
 
 // dQ: waves of 32 packed rows over the keys, as the forward pass.
 //   S^T = K Q^T, dP^T = V dO^T, dS^T = P^T (dP^T - delta), dQ^T += K^T dS^T,
-// with delta = sum_d dO out per row.  For the kernel of dK and dV, which runs
-// next, it leaves delta, and lse in base 2 (infinite where the row sees no
-// key, so that its probabilities come out zero).
+// with delta = sum_d dO out = sum_j P dP per row.  For the kernel of dK and dV,
+// which runs next, it leaves delta, and lse in base 2 (infinite where the row
+// sees no key, so that its probabilities come out zero).
+//
+// Of 16-bit types the stored out has been rounded, and where a row averages
+// few values that shows in delta and then in all gradients (errors of dk against
+// 64 bits over that of its own last rounding: 7 causal sequences up to 989 rows
+// 1.52, 12 of up to 11 rows 2.13).  Tiles of rows that see up to kExactKeys
+// keys therefore take the sum over keys first, in two more products (1.41 and
+// 1.44); what is left are the roundings of P and dS, as operands of their
+// products, and of the outputs.
+constexpr int kExactKeys = 512;
 template <class T, int D, int NW, int BN>
 __global__ __launch_bounds__(NW * 64, (Plan<T, D>::kDqWaves)) void k_attention_dq(AttnArgs a) {
   using L = Tile<T, D, BN>;
@@ -744,7 +754,7 @@ __global__ __launch_bounds__(NW * 64, (Plan<T, D>::kDqWaves)) void k_attention_d
   __shared__ __attribute__((aligned(16))) char lds[2][2][L::kBytes];
   const Item item(a);
   const int kvh = item.kvh;
-  const Place p = place_of(a.q_off, a.n_seq, a.n_q, a.group, BM, item.tile, item.tiles);
+  const Place p = place_of(a.q_off, a.n_seq, a.n_q, a.group, BM, item.tile, item.tiles, true);
   if (p.s < 0) return;
   const Seq e = seq_of(a, p.s);
   const int rows = e.lq * a.group;
@@ -752,7 +762,8 @@ __global__ __launch_bounds__(NW * 64, (Plan<T, D>::kDqWaves)) void k_attention_d
   const int r0 = p.at * BM;
   const int w = wave(), l32 = lane() & 31, h = lane() >> 5;
   const int last = r0 + BM < rows ? r0 + BM - 1 : rows - 1;
-  int t0 = 0, t1 = (seen_keys(a, e, last) + BN - 1) / BN;
+  const int most = seen_keys(a, e, last);
+  int t0 = 0, t1 = (most + BN - 1) / BN;
   if (a.n_split > 1) {
     const int per = (t1 + a.n_split - 1) / a.n_split;
     t0 = item.part * per;
@@ -778,21 +789,8 @@ __global__ __launch_bounds__(NW * 64, (Plan<T, D>::kDqWaves)) void k_attention_d
     qf[i] = global_frag<T>(qp, true, 16 * i, a.dim);
     df[i] = global_frag<T>(dp, true, 16 * i, a.dim);
   }
-  const T* op = (const T*)a.out + at * a.dim;
-  float delta = 0.f;
-#pragma unroll
-  for (int i = 0; i < D / 16; ++i) {
-    const frag_t<T> of = global_frag<T>(op, true, 16 * i, a.dim);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) delta += (float)of[j] * (float)df[i][j];
-  }
-  delta = half_sum(delta);
   float lse2 = a.lse[at];
   lse2 = lse2 == -OC_INF ? OC_INF : lse2 * kLog2e;
-  if (item.part == 0 && h == 0 && r < rows) {
-    a.delta[at] = delta;
-    a.lse2[at] = lse2;
-  }
   f32x16 g[D / 32];
   const float c = a.scale * kLog2e;
 
@@ -802,13 +800,51 @@ __global__ __launch_bounds__(NW * 64, (Plan<T, D>::kDqWaves)) void k_attention_d
     stage.copy(lds[b][0], k + j * a.k_row, a.k_row, e.lk - (int)j, a.dim);
     stage.copy(lds[b][1], v + j * a.v_row, a.v_row, e.lk - (int)j, a.dim);
   };
+  typename L::Lanes ln;
+
+  float delta = 0.f;
+  if (sizeof(T) == 2 && most <= kExactKeys) {
+    if (most > 0) load(0, 0);
+    wait_copies();
+    for (int t = 0; t * BN < most; ++t) {
+      ln.renew();
+      if ((t + 1) * BN < most) load(t + 1, (t + 1) & 1);
+#pragma unroll
+      for (int n = 0; n < BN / 32; ++n) {
+        f32x16 x = zero16(), y = zero16();
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) x = mma(L::rows(lds[t & 1][0], ln, 32 * n, 16 * i), qf[i], x);
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) y = mma(L::rows(lds[t & 1][1], ln, 32 * n, 16 * i), df[i], y);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int key = t * BN + 32 * n + 8 * (i / 4) + 4 * h + i % 4;
+          const float pr = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], c, -lse2)) * y[i];
+          delta += key >= seen ? 0.f : pr;
+        }
+      }
+      wait_copies();
+    }
+  } else {
+    const T* op = (const T*)a.out + at * a.dim;
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) {
+      const frag_t<T> of = global_frag<T>(op, true, 16 * i, a.dim);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) delta += (float)of[j] * (float)df[i][j];
+    }
+  }
+  delta = half_sum(delta);
+  if (item.part == 0 && h == 0 && r < rows) {
+    a.delta[at] = delta;
+    a.lse2[at] = lse2;
+  }
 #pragma unroll
   for (int d = 0; d < D / 32; ++d) g[d] = zero16();
   const int edge = a.causal ? seen_keys(a, e, r0) / BN : t1;
   bool found = false;
   if (t0 < t1) load(t0, 0);
   wait_copies();
-  typename L::Lanes ln;
   for (int t = t0; t < t1; ++t) {
     ln.renew();
     char* kt = lds[(t - t0) & 1][0];
@@ -872,7 +908,7 @@ __global__ __launch_bounds__(NW * 64, (Plan<T, D>::kDkvWaves)) void k_attention_
   __shared__ __attribute__((aligned(16))) char vt[kLds ? LK::kBytes : 16];
   const Item item(a);
   const int kvh = item.kvh;
-  const Place p = place_of(a.k_off, a.n_seq, a.n_k, 1, BK, item.tile, item.tiles);
+  const Place p = place_of(a.k_off, a.n_seq, a.n_k, 1, BK, item.tile, item.tiles, false);
   if (p.s < 0) return;
   const Seq e = seq_of(a, p.s);
   // Early keys are seen by the most rows.

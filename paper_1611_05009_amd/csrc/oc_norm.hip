@@ -110,9 +110,11 @@ __global__ __launch_bounds__(WIDE ? 1024 : 256) void k_rms_norm(NormArgs a) {
     if constexpr (sizeof(TY) == 1) {
       // The row's largest value stands at 448, the largest of the 8-bit type.
       most = row_reduce<WIDE, true>(most, lanes, part);
-      const float scale = most > 0.f ? most / 448.f : 1.f, inv = 1.f / scale;
+      // Divided by: a product with the reciprocal puts more values on the
+      // other side of a rounding's middle.
+      const float scale = most > 0.f ? most / 448.f : 1.f;
 #pragma unroll
-      for (int v = 0; v < NV; ++v) x[v] *= inv;
+      for (int v = 0; v < NV; ++v) x[v] /= scale;
       if (live && col.t == 0) a.scale[row] = scale;
     }
     if (live) {
