@@ -37,8 +37,15 @@ constexpr float kLn2 = 0.6931471805599453f;
 #define OC_INF __builtin_inff()
 
 // Fragment of eight contraction elements per lane, and one 32x32 product over
-// 16 of them: one instruction for 16-bit types; for float eight
-// instructions that contract elements (i of half 0, i of half 1) each.
+// 16 of them.  16-bit types: one instruction.  float: three bfloat16 terms of
+// eight bits each, cut off one after the other, which are the number exactly;
+// of the nine products the six of 2^-16 and above, smallest first.  They take
+// 6 x 32 cycles where the 32-bit matrix instructions take 8 x 64, and what they
+// leave out is below the last bit of a 32-bit product.  (Infinite elements
+// come out as NaN in their products.)
+struct Terms {
+  bf16x8 a, b, c;
+};
 template <class T>
 struct Frag;
 template <>
@@ -55,7 +62,7 @@ struct Frag<_Float16> {
 };
 template <>
 struct Frag<float> {
-  using type = f32x8;
+  using type = Terms;
   static constexpr int kShift = 0;
 };
 template <class T>
@@ -67,10 +74,39 @@ __device__ __forceinline__ f32x16 mma(bf16x8 a, bf16x8 b, f32x16 c) {
 __device__ __forceinline__ f32x16 mma(f16x8 a, f16x8 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
 }
-__device__ __forceinline__ f32x16 mma(f32x8 a, f32x8 b, f32x16 c) {
+__device__ __forceinline__ f32x16 mma(const Terms& x, const Terms& y, f32x16 c) {
+  c = mma(x.c, y.a, c);
+  c = mma(x.a, y.c, c);
+  c = mma(x.b, y.b, c);
+  c = mma(x.b, y.a, c);
+  c = mma(x.a, y.b, c);
+  return mma(x.a, y.a, c);
+}
+
+// The upper halves of eight words, and the words without them.
+__device__ __forceinline__ bf16x8 cut(f32x8& x) {
+  u32x4 r;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], b[i], c, 0, 0, 0);
-  return c;
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t lo = __float_as_uint(x[2 * i]), hi = __float_as_uint(x[2 * i + 1]);
+    r[i] = __builtin_amdgcn_perm(hi, lo, 0x07060302);
+    x[2 * i] -= __uint_as_float(lo & 0xffff0000u);
+    x[2 * i + 1] -= __uint_as_float(hi & 0xffff0000u);
+  }
+  return __builtin_bit_cast(bf16x8, r);
+}
+
+template <class T>
+__device__ __forceinline__ frag_t<T> pack(f32x8 x) {
+  if constexpr (sizeof(T) == 4) {
+    Terms f;
+    f.a = cut(x);
+    f.b = cut(x);
+    f.c = cut(x);
+    return f;
+  } else {
+    return __builtin_convertvector(x, frag_t<T>);
+  }
 }
 
 __device__ __forceinline__ int lane() { return (int)(threadIdx.x & 63); }
@@ -113,7 +149,7 @@ __device__ __forceinline__ frag_t<T> to_frag(const f32x16& c, int first) {
   f32x8 x;
 #pragma unroll
   for (int i = 0; i < 8; ++i) x[i] = c[first + i];
-  return __builtin_convertvector(x, frag_t<T>);
+  return pack<T>(x);
 }
 
 // A tile of R rows of up to D elements in LDS: rows of P elements (P the
@@ -126,7 +162,7 @@ __device__ __forceinline__ frag_t<T> to_frag(const f32x16& c, int first) {
 // one chunk further.  Changing places by four bits of the row does the same,
 // but leaves twice as many addresses in registers, which the gradients do not
 // have.  (Before, LDS was busy half of the time at head size 128, and half of
-// that with conflicts.)  32-bit products take 16 times as long, and their
+// that with conflicts.)  32-bit products take six times as long, and their
 // reads need no such care.
 template <class T, int D, int R>
 struct Tile {
@@ -191,7 +227,7 @@ struct Tile {
       const int r = lane() & 31, h = lane() >> 5;
       const f32x4 x = *(const f32x4*)(t + at(row, r, col / 4 + 2 * h));
       const f32x4 y = *(const f32x4*)(t + at(row, r, col / 4 + 2 * h + 1));
-      return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+      return pack<T>(__builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
     }
   }
 
@@ -212,7 +248,7 @@ struct Tile {
       f32x8 x;
 #pragma unroll
       for (int i = 0; i < 8; ++i) x[i] = *(const float*)(t + at(row, 8 * (i / 4) + 4 * h + i % 4, c / 4) + (c & 3) * 4);
-      return x;
+      return pack<T>(x);
     }
   }
 };
@@ -431,16 +467,19 @@ __device__ __forceinline__ u32x4 load16(const T* p) {
 
 // B fragment (elements col + 8 h .. of a row in global memory), zero past dim.
 template <class T>
-__device__ __forceinline__ frag_t<T> global_frag(const T* row, bool valid, int col, int dim) {
+__device__ __forceinline__ f32x8 global8(const T* row, int col, int dim) {
   const int c = col + 8 * (lane() >> 5);
+  const u32x4 z = {0, 0, 0, 0}, x = c < dim ? load16(row + c) : z, y = c + 4 < dim ? load16(row + c + 4) : z;
+  return __builtin_shufflevector(__builtin_bit_cast(f32x4, x), __builtin_bit_cast(f32x4, y), 0, 1, 2, 3, 4, 5, 6, 7);
+}
+template <class T>
+__device__ __forceinline__ frag_t<T> global_frag(const T* row, bool valid, int col, int dim) {
   if constexpr (sizeof(T) == 2) {
+    const int c = col + 8 * (lane() >> 5);
     const u32x4 x = valid && c < dim ? load16(row + c) : u32x4{0, 0, 0, 0};
     return __builtin_bit_cast(frag_t<T>, x);
   } else {
-    const u32x4 z = {0, 0, 0, 0};
-    const u32x4 x = valid && c < dim ? load16(row + c) : z;
-    const u32x4 y = valid && c + 4 < dim ? load16(row + c + 4) : z;
-    return __builtin_shufflevector(__builtin_bit_cast(f32x4, x), __builtin_bit_cast(f32x4, y), 0, 1, 2, 3, 4, 5, 6, 7);
+    return pack<T>(global8(row, col, valid ? dim : 0));
   }
 }
 
@@ -465,8 +504,8 @@ __device__ __forceinline__ void store_col(T* p, const f32x16& c, int d0, int dim
 // forward pass measured 488 TFLOP/s with one and 727 with two.  The steps are the
 // largest whose two buffers leave LDS, and whose fragments leave registers, for
 // the second wave; dK and dV at head sizes over 64 also need the values in LDS
-// instead of registers for that (503 to 774 TFLOP/s).  32-bit fragments are
-// twice as large and leave room for one wave in the gradients.
+// instead of registers for that (503 to 774 TFLOP/s).  The three terms
+// of 32-bit fragments leave room for one wave in the gradients' wide heads.
 template <class T, int D>
 struct Plan {
   static constexpr bool kWide = D > 64, kHalf = sizeof(T) == 2;
@@ -829,9 +868,15 @@ __global__ __launch_bounds__(NW * 64, (Plan<T, D>::kDqWaves)) void k_attention_d
     const T* op = (const T*)a.out + at * a.dim;
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) {
-      const frag_t<T> of = global_frag<T>(op, true, 16 * i, a.dim);
+      if constexpr (sizeof(T) == 2) {
+        const frag_t<T> of = global_frag<T>(op, true, 16 * i, a.dim);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) delta += (float)of[j] * (float)df[i][j];
+        for (int j = 0; j < 8; ++j) delta += (float)of[j] * (float)df[i][j];
+      } else {
+        const f32x8 x = global8(op, 16 * i, a.dim) * global8(dp, 16 * i, a.dim);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) delta += x[j];
+      }
     }
   }
   delta = half_sum(delta);
@@ -1119,11 +1164,10 @@ static int parts_of(int64_t workgroups, int64_t wanted, int64_t steps, int64_t l
 
 // The device holds two workgroups per CU.  Parts cost a write and a read of
 // float rows each, so in 16 bits only grids under half of the device are split;
-// 32-bit steps take 16 times as long and are worth it up to all of it (8192 rows
-// causal, 4 heads of 32: 316 us in one part, 186 in four).  Single steps are not
-// (937 rows, 4 heads of 64 over 2, with gradients: 97 us, in single steps 122).
-// Sequences whose rows fit one wave (single tokens) only
-// stream their keys: many short parts keep the loads going and even out the
+// 32-bit steps take six times as long and are worth it up to all of it (8192
+// rows causal, 4 heads of 32: 276 us in one part, 134 in four).  Single steps
+// are not (937 rows, 4 heads of 64 over 2: 29 us in double steps, 37 in single
+// X and even out the
 // lengths (32 sequences of up to 8192 keys: 302 us in one part, 135 in eight).
 static int row_parts(int64_t workgroups, int64_t steps, int dtype) {
   if (dtype == kF32) return workgroups > 512 ? 1 : parts_of(workgroups, 1024, steps, 2);
