@@ -17,8 +17,8 @@
 // already the B operand of O^T = V^T P^T.  The A operand takes its keys in
 // the same order: element i of lane half h is key 8 (i / 4) + 4 h + i % 4 of
 // each 16.  Softmax statistics are per lane, with one exchange between lane
-// halves per tile.  16-bit A operands over the row index of an LDS tile come
-// from the transposing LDS read; 32-bit ones are read one by one.
+// halves per tile.  A operands over the row index of an LDS tile come from the
+// transposing LDS read.
 #include "oc_attention.h"
 
 namespace oci {
@@ -41,8 +41,9 @@ constexpr float kLn2 = 0.6931471805599453f;
 // eight bits each, cut off one after the other, which are the number exactly;
 // of the nine products the six of 2^-16 and above, smallest first.  They take
 // 6 x 32 cycles where the 32-bit matrix instructions take 8 x 64, and what they
-// leave out is below the last bit of a 32-bit product.  (Infinite elements
-// come out as NaN in their products.)
+// leave out is below the last bit of a 32-bit product.  (8192 keys, 8 heads of
+// 96: forward 1574 us with those instructions, 970 with terms.)  Infinite elements
+// come out as NaN in their products.
 struct Terms {
   bf16x8 a, b, c;
 };
@@ -162,37 +163,22 @@ __device__ __forceinline__ frag_t<T> to_frag(const f32x16& c, int first) {
 // one chunk further.  Changing places by four bits of the row does the same,
 // but leaves twice as many addresses in registers, which the gradients do not
 // have.  (Before, LDS was busy half of the time at head size 128, and half of
-// that with conflicts.)  32-bit products take six times as long, and their
-// reads need no such care.
+// that with conflicts.)
 template <class T, int D, int R>
 struct Tile {
-  static constexpr int kPer = 16 / (int)sizeof(T);        // elements per chunk
+  static_assert(sizeof(T) == 2, "float: below");
+  static constexpr int kPer = 8;                          // elements per chunk
   static constexpr int P = D <= 32 ? 32 : D <= 64 ? 64 : 128;
-  static constexpr int kChunks = P / kPer;                // chunks per row: 4, 8, 16 or 32
+  static constexpr int kChunks = P / kPer;                // chunks per row: 4, 8 or 16
   static constexpr int kGroup = 64 / kChunks;             // rows of a group
-  static constexpr int kPad = sizeof(T) == 2 && kChunks >= 8 ? 16 : 0;
+  static constexpr int kPad = kChunks >= 8 ? 16 : 0;
   static constexpr int kBytes = R / kGroup * (1024 + kPad);
   static_assert(R % 16 == 0, "whole fragments");
 
   static __device__ __forceinline__ int swizzle(int r) {
-    if constexpr (sizeof(T) == 4) return ((r & 3) << 1) | ((r >> 2) & 1);
     if constexpr (kChunks == 4) return (r >> 2) & 3;
     if constexpr (kChunks == 8) return ((r << 1) & 4) | ((r >> 1) & 2);
     return (r & 3) << 2;
-  }
-  static __device__ __forceinline__ int at(int r, int chunk) {
-    return r * (kChunks * 16) + r / kGroup * kPad + (chunk ^ swizzle(r)) * 16;
-  }
-  // The same for `row` + r, row a multiple of 16.
-  static __device__ __forceinline__ int at(int row, int r, int chunk) {
-    return row * (kChunks * 16) + row / kGroup * kPad + at(r, chunk);
-  }
-
-  static __device__ __forceinline__ float get(const char* t, int r, int c) {
-    return (float)*(const T*)(t + at(r, c / kPer) + c % kPer * (int)sizeof(T));
-  }
-  static __device__ __forceinline__ void clear(char* t, int r, int c) {
-    *(T*)(t + at(r, c / kPer) + c % kPer * (int)sizeof(T)) = (T)0.f;
   }
 
   // This lane's part of its addresses: those of a row-wise read start at
@@ -219,37 +205,38 @@ struct Tile {
 
   // Elements 8 h .. 8 h + 7 past `col` of row `row + lane % 32`.
   static __device__ __forceinline__ frag_t<T> rows(const char* t, const Lanes& a, int row, int col) {
-    if constexpr (sizeof(T) == 2) {
-      const int c = col * 2;
-      const u32x4 x = *(const u32x4*)(t + a.row_at + (a.row_x ^ (c & kSwaps)) + (row_offset(row) + (c & ~kSwaps)));
-      return __builtin_bit_cast(frag_t<T>, x);
-    } else {
-      const int r = lane() & 31, h = lane() >> 5;
-      const f32x4 x = *(const f32x4*)(t + at(row, r, col / 4 + 2 * h));
-      const f32x4 y = *(const f32x4*)(t + at(row, r, col / 4 + 2 * h + 1));
-      return pack<T>(__builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
-    }
+    const int c = col * 2;
+    const u32x4 x = *(const u32x4*)(t + a.row_at + (a.row_x ^ (c & kSwaps)) + (row_offset(row) + (c & ~kSwaps)));
+    return __builtin_bit_cast(frag_t<T>, x);
   }
 
   // Rows row + 8 (i / 4) + 4 h + i % 4, i = 0..7, of column col + lane % 32.
   static __device__ __forceinline__ frag_t<T> cols(const char* t, const Lanes& a, int row, int col) {
-    if constexpr (sizeof(T) == 2) {
-      using lds4 = __attribute__((address_space(3))) i16x4;
-      const int c = col * 2;
-      const char* p = t + a.col_at + (row_offset(row) + (c & ~kSwaps));
-      const char* q = p + (a.col_x ^ (c & kSwaps));
-      // Eight rows on, a line of four rows swaps by another number.
-      const char* q8 = kChunks == 4 ? p + (a.col_x ^ (c & kSwaps) ^ 0x20) : q;
-      const i16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)q);
-      const i16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(q8 + row_offset(8)));
-      return __builtin_bit_cast(frag_t<T>, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
-    } else {
-      const int c = col + (lane() & 31), h = lane() >> 5;
-      f32x8 x;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = *(const float*)(t + at(row, 8 * (i / 4) + 4 * h + i % 4, c / 4) + (c & 3) * 4);
-      return pack<T>(x);
-    }
+    using lds4 = __attribute__((address_space(3))) i16x4;
+    const int c = col * 2;
+    const char* p = t + a.col_at + (row_offset(row) + (c & ~kSwaps));
+    const char* q = p + (a.col_x ^ (c & kSwaps));
+    // Eight rows on, a line of four rows swaps by another number.
+    const char* q8 = kChunks == 4 ? p + (a.col_x ^ (c & kSwaps) ^ 0x20) : q;
+    const i16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)q);
+    const i16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(q8 + row_offset(8)));
+    return __builtin_bit_cast(frag_t<T>, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+  }
+};
+
+// float: a tile of each of the three terms.
+template <int D, int R>
+struct Tile<float, D, R> : Tile<__bf16, D, R> {
+  using Term = Tile<__bf16, D, R>;
+  using Lanes = typename Term::Lanes;
+  static constexpr int kBytes = 3 * Term::kBytes;
+  static __device__ __forceinline__ Terms rows(const char* t, const Lanes& a, int row, int col) {
+    return Terms{Term::rows(t, a, row, col), Term::rows(t + Term::kBytes, a, row, col),
+                 Term::rows(t + 2 * Term::kBytes, a, row, col)};
+  }
+  static __device__ __forceinline__ Terms cols(const char* t, const Lanes& a, int row, int col) {
+    return Terms{Term::cols(t, a, row, col), Term::cols(t + Term::kBytes, a, row, col),
+                 Term::cols(t + 2 * Term::kBytes, a, row, col)};
   }
 };
 
@@ -259,13 +246,20 @@ __device__ __forceinline__ int by_group(const AttnArgs& a, int n) {
 }
 
 // Rows past the end and columns past the head size are copied from here.
-__device__ const u32x4 kZeros = {0, 0, 0, 0};
+__device__ const u32x4 kZeros[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
 
 // Copy of tiles from global memory straight into LDS.  A wave's 64 chunks land
 // one after the other, so the chunk that belongs at a position is what each
-// lane asks for.  A copy is asynchronous until the next wait_copies().
+// lane asks for.  A copy is asynchronous until the next wait_copies(), so
+// while one buffer is read the next one is filled.
+// float is cut into its terms on the way, once for the whole workgroup, and so
+// comes through registers (Held): copy() starts the loads and store() puts
+// them into the one buffer, when no wave reads it any more.  (Cut by each wave
+// as it reads: forward of 4096 keys, 16 heads of 128 over 4, causal, 606 us, so 453.)
 template <class T, int D, int R, int NT>
 struct Stage {
+  static constexpr bool kDirect = sizeof(T) == 2;
+  static constexpr int kBuffers = kDirect ? 2 : 1;
   using L = Tile<T, D, R>;
   static constexpr int kN = R * L::kChunks / NT;    // chunks per thread
   static constexpr int kStep = NT / L::kChunks;     // rows between them
@@ -281,7 +275,15 @@ struct Stage {
     return (chunk ^ L::swizzle(kStep % 8 ? row + i * kStep : row)) * L::kPer;
   }
 
-  static __device__ __forceinline__ void put(char* t, int i, const void* p) {
+  struct Held {
+    f32x8 x[kDirect ? 1 : kN];
+  };
+  static __device__ __forceinline__ void put(char* t, Held& held, int i, const T* p) {
+    if (!p) p = (const T*)kZeros;
+    if constexpr (!kDirect) {
+      held.x[i] = *(const f32x8*)p;
+      return;
+    }
     char* to = t + (wave() + i * (NT / 64)) * (1024 + L::kPad);
     const uint32_t at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)to;
     // As an instruction of its own: for the builtin the compiler waits for the
@@ -290,18 +292,30 @@ struct Stage {
     // the write of m0 to its use.)
     asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"{m0}"(at), "v"(p) : "memory");
   }
+  static __device__ __forceinline__ void store(char* t, Held& held) {
+    if constexpr (!kDirect) {
+#pragma unroll
+      for (int i = 0; i < kN; ++i) {
+        char* to = t + (wave() + i * (NT / 64)) * (1024 + L::kPad) + lane() * 16;
+        const Terms x = pack<float>(held.x[i]);
+        *(bf16x8*)to = x.a;
+        *(bf16x8*)(to + L::kBytes / 3) = x.b;
+        *(bf16x8*)(to + 2 * (L::kBytes / 3)) = x.c;
+      }
+    }
+  }
 
   // R rows from p on, `stride` elements apart, of which `rows` exist.
-  __device__ __forceinline__ void copy(char* t, const T* p, int64_t stride, int rows, int dim) const {
+  __device__ __forceinline__ void copy(char* t, Held& held, const T* p, int64_t stride, int rows, int dim) const {
     const T* q = p + row * stride;
     if (rows >= R && dim == D) {
 #pragma unroll
-      for (int i = 0; i < kN; ++i) put(t, i, q + i * kStep * stride + col(i));
+      for (int i = 0; i < kN; ++i) put(t, held, i, q + i * kStep * stride + col(i));
     } else {
 #pragma unroll
       for (int i = 0; i < kN; ++i) {
         const bool in = (col(i) < dim) & (row + i * kStep < rows);
-        put(t, i, in ? (const void*)(q + i * kStep * stride + col(i)) : (const void*)&kZeros);
+        put(t, held, i, in ? q + i * kStep * stride + col(i) : nullptr);
       }
     }
   }
@@ -309,14 +323,15 @@ struct Stage {
   // Packed rows r .. r + R - 1 of two arrays, of which those below `rows`
   // exist; offset_x and offset_y map (query, head of the group) to elements.
   template <class A, class X, class Y>
-  __device__ __forceinline__ void copy_packed(char* tx, char* ty, const A& a, int r, int rows, X at_x, Y at_y) const {
+  __device__ __forceinline__ void copy_packed(char* tx, Held& hx, char* ty, Held& hy, const A& a, int r, int rows,
+                                              X at_x, Y at_y) const {
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
       const int n = r + row + i * kStep;
       const bool in = (col(i) < a.dim) & (n < rows);
       const int q = by_group(a, n), g = n - q * a.group;
-      put(tx, i, in ? (const void*)(at_x(q, g) + col(i)) : (const void*)&kZeros);
-      put(ty, i, in ? (const void*)(at_y(q, g) + col(i)) : (const void*)&kZeros);
+      put(tx, hx, i, in ? at_x(q, g) + col(i) : nullptr);
+      put(ty, hy, i, in ? at_y(q, g) + col(i) : nullptr);
     }
   }
 };
@@ -502,19 +517,29 @@ __device__ __forceinline__ void store_col(T* p, const f32x16& c, int d0, int dim
 // Step sizes and waves per SIMD by type and head size.  Two waves of a SIMD
 // cover each other's softmax and LDS reads: at head size 128 in bfloat16 the
 // forward pass measured 488 TFLOP/s with one and 727 with two.  The steps are the
-// largest whose two buffers leave LDS, and whose fragments leave registers, for
-// the second wave; dK and dV at head sizes over 64 also need the values in LDS
-// instead of registers for that (503 to 774 TFLOP/s).  The three terms
-// of 32-bit fragments leave room for one wave in the gradients' wide heads.
+// largest whose buffers leave LDS, and whose fragments leave registers, for the
+// second wave; dK and dV at head sizes over 64, and in float at all, also need
+// the values in LDS instead of registers for that (503 to 774 TFLOP/s; all
+// gradients of 4096 float rows, 8 heads of 64: 785 to 680 us).  The three terms of
+// float fragments leave room for one wave in the gradients' wide heads.
+//
+// The wave that is past its first product goes first until the end of its step
+// (s_setprio), so that the two do not wait for the same units all the time.  In
+// the gradients that gains 1 to 3%; forward (kFirst), in us without and with:
+// bfloat16, 16384 keys of 4 heads of 32: 232, 222; 8192 of 8 of 96: 232, 219; 8192
+// causal, 16 of 128 over 4: 293, 264; but 8192 causal, 8 of 64: 127, 137.  float,
+// 4096 of 8 of 64: 189, 181; 8192 of 8 of 96: 1031, 970; 8192 causal, 4 of 32: 109,
+// 110; but 4096 causal, 16 of 128 over 4: 437, 465.
 template <class T, int D>
 struct Plan {
   static constexpr bool kWide = D > 64, kHalf = sizeof(T) == 2;
   static constexpr int kKeys = kHalf && D <= 32 ? 128 : kHalf || !kWide ? 64 : 32;  // forward
-  static constexpr int kDqKeys = kHalf ? 64 : 32;
+  static constexpr bool kFirst = kHalf ? D != 64 : D == 64 || D == 96;
+  static constexpr int kDqKeys = kHalf || !kWide ? 64 : 32;
   static constexpr int kDqWaves = kHalf || !kWide ? 2 : 1;
-  static constexpr int kDkvRows = kHalf && !kWide ? 64 : 32;
-  static constexpr int kDkvWaves = kHalf || D <= 32 ? 2 : 1;
-  static constexpr bool kValuesInLds = kHalf && kWide;
+  static constexpr int kDkvRows = (kHalf && !kWide) || D <= 32 ? 64 : 32;
+  static constexpr int kDkvWaves = kHalf || !kWide ? 2 : 1;
+  static constexpr bool kValuesInLds = !kHalf || kWide;
 };
 
 // ---------------------------------------------------------------------------
@@ -533,16 +558,13 @@ __device__ __forceinline__ bool is_finite(float x) { return x - x == 0.f; }
 
 // The bits of a word that are the signs of its elements whose exponent is all
 // ones, and zeros in the place of those elements.
+// (Those of a float are in its first term.)
 template <class T>
 __device__ __forceinline__ uint32_t not_finite(uint32_t x) {
-  if constexpr (sizeof(T) == 4) return ((x & 0x7f800000u) + 0x00800000u) & 0x80000000u;
-  if constexpr (std::is_same<T, __bf16>::value) return ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+  if constexpr (!std::is_same<T, _Float16>::value) return ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
   return ((x & 0x7c007c00u) + 0x04000400u) & 0x80008000u;
 }
-template <class T>
-__device__ __forceinline__ uint32_t without(uint32_t x, uint32_t signs) {
-  return x & ~(sizeof(T) == 4 ? (uint32_t)((int32_t)signs >> 31) : (signs >> 15) * 0xffffu);
-}
+__device__ __forceinline__ uint32_t without(uint32_t x, uint32_t signs) { return x & ~((signs >> 15) * 0xffffu); }
 
 // By the whole workgroup, a barrier at its end; true if anything was found.
 template <class T, int D, int R, int NT>
@@ -556,7 +578,17 @@ __device__ __forceinline__ bool clean(char* tile) {
     const uint32_t any = not_finite<T>(x[0]) | not_finite<T>(x[1]) | not_finite<T>(x[2]) | not_finite<T>(x[3]);
     if (any) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = without<T>(x[i], not_finite<T>(x[i]));
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t signs = not_finite<T>(x[i]);
+        x[i] = without(x[i], signs);
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+          for (int term = 1; term < 3; ++term) {
+            uint32_t* y = (uint32_t*)((char*)p + term * (L::kBytes / 3)) + i;
+            *y = without(*y, signs);
+          }
+        }
+      }
       *p = x;
       found = true;
     }
@@ -596,7 +628,8 @@ template <class T, int D, int NW, int BN>
 __global__ __launch_bounds__(NW * 64, 2) void k_attention(AttnArgs a) {
   using L = Tile<T, D, BN>;
   constexpr int NT = NW * 64, BM = NW * 32;
-  __shared__ __attribute__((aligned(16))) char lds[2][2][L::kBytes];
+  using S = Stage<T, D, BN, NT>;
+  __shared__ __attribute__((aligned(16))) char lds[S::kBuffers][2][L::kBytes];
 
   const Item item(a);
   const int kvh = item.kvh;
@@ -634,11 +667,12 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention(AttnArgs a) {
   for (int i = 0; i < D / 16; ++i) qf[i] = global_frag<T>(qp, true, 16 * i, a.dim);
   const float c = a.scale * kLog2e;
 
-  const Stage<T, D, BN, NT> stage;
+  const S stage;
+  typename S::Held hk, hv;
   const auto load = [&](int t, int b) {
     const int64_t j = (int64_t)t * BN;
-    stage.copy(lds[b][0], k + j * a.k_row, a.k_row, e.lk - (int)j, a.dim);
-    stage.copy(lds[b][1], v + j * a.v_row, a.v_row, e.lk - (int)j, a.dim);
+    stage.copy(lds[b][0], hk, k + j * a.k_row, a.k_row, e.lk - (int)j, a.dim);
+    stage.copy(lds[b][1], hv, v + j * a.v_row, a.v_row, e.lk - (int)j, a.dim);
   };
   f32x16 o[D / 32];
   float mx = -OC_INF, sum = 0.f;
@@ -647,14 +681,19 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention(AttnArgs a) {
   // First step that hides a key from a row of the workgroup.
   const int edge = a.causal ? seen_keys(a, e, r0) / BN : t1;
   bool found = false;
-  if (t0 < t1) load(t0, 0);
+  if (t0 < t1) {
+    load(t0, 0);
+    S::store(lds[0][0], hk);
+    S::store(lds[0][1], hv);
+  }
   wait_copies();
   typename L::Lanes ln;
   for (int t = t0; t < t1; ++t) {
     ln.renew();
-    const char* kt = lds[(t - t0) & 1][0];
-    char* vt = lds[(t - t0) & 1][1];
-    if (t + 1 < t1) load(t + 1, (t + 1 - t0) & 1);
+    const int b = (t - t0) % S::kBuffers;
+    const char* kt = lds[b][0];
+    char* vt = lds[b][1];
+    if (t + 1 < t1) load(t + 1, S::kBuffers - 1 - b);
     if (t >= edge) found |= clean<T, D, BN, NT>(vt);
     if (t * BN < seen_max) {
       f32x16 x[BN / 32];
@@ -666,6 +705,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention(AttnArgs a) {
       }
       // 907 to 924 TFLOP/s at head size 128; smaller ones gain nothing.
       if constexpr (sizeof(T) == 2 && D > 64) pace<4, BN / 32 * (D / 16) - 4, 1, 4>();
+      if constexpr (Plan<T, D>::kFirst) __builtin_amdgcn_s_setprio(1);
       if ((t + 1) * BN > seen_min) {
 #pragma unroll
         for (int n = 0; n < BN / 32; ++n)
@@ -711,6 +751,14 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attention(AttnArgs a) {
 #pragma unroll
           for (int d = 0; d < D / 32; ++d) o[d] = mma(L::cols(vt, ln, 32 * n + 16 * j, 32 * d), pf, o[d]);
         }
+      if constexpr (Plan<T, D>::kFirst) __builtin_amdgcn_s_setprio(0);
+    }
+    if constexpr (!S::kDirect) {
+      __syncthreads();
+      if (t + 1 < t1) {
+        S::store(lds[0][0], hk);
+        S::store(lds[0][1], hv);
+      }
     }
     wait_copies();
   }
@@ -790,7 +838,8 @@ template <class T, int D, int NW, int BN>
 __global__ __launch_bounds__(NW * 64, (Plan<T, D>::kDqWaves)) void k_attention_dq(AttnArgs a) {
   using L = Tile<T, D, BN>;
   constexpr int NT = NW * 64, BM = NW * 32;
-  __shared__ __attribute__((aligned(16))) char lds[2][2][L::kBytes];
+  using S = Stage<T, D, BN, NT>;
+  __shared__ __attribute__((aligned(16))) char lds[S::kBuffers][2][L::kBytes];
   const Item item(a);
   const int kvh = item.kvh;
   const Place p = place_of(a.q_off, a.n_seq, a.n_q, a.group, BM, item.tile, item.tiles, true);
@@ -833,16 +882,19 @@ __global__ __launch_bounds__(NW * 64, (Plan<T, D>::kDqWaves)) void k_attention_d
   f32x16 g[D / 32];
   const float c = a.scale * kLog2e;
 
-  const Stage<T, D, BN, NT> stage;
+  const S stage;
+  typename S::Held hk, hv;
   const auto load = [&](int t, int b) {
     const int64_t j = (int64_t)t * BN;
-    stage.copy(lds[b][0], k + j * a.k_row, a.k_row, e.lk - (int)j, a.dim);
-    stage.copy(lds[b][1], v + j * a.v_row, a.v_row, e.lk - (int)j, a.dim);
+    stage.copy(lds[b][0], hk, k + j * a.k_row, a.k_row, e.lk - (int)j, a.dim);
+    stage.copy(lds[b][1], hv, v + j * a.v_row, a.v_row, e.lk - (int)j, a.dim);
   };
   typename L::Lanes ln;
 
   float delta = 0.f;
-  if (sizeof(T) == 2 && most <= kExactKeys) {
+  bool exact = false;
+  if constexpr (S::kDirect) exact = most <= kExactKeys;
+  if (exact) {
     if (most > 0) load(0, 0);
     wait_copies();
     for (int t = 0; t * BN < most; ++t) {
@@ -852,9 +904,9 @@ __global__ __launch_bounds__(NW * 64, (Plan<T, D>::kDqWaves)) void k_attention_d
       for (int n = 0; n < BN / 32; ++n) {
         f32x16 x = zero16(), y = zero16();
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i) x = mma(L::rows(lds[t & 1][0], ln, 32 * n, 16 * i), qf[i], x);
+        for (int i = 0; i < D / 16; ++i) x = mma(L::rows(lds[t % S::kBuffers][0], ln, 32 * n, 16 * i), qf[i], x);
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i) y = mma(L::rows(lds[t & 1][1], ln, 32 * n, 16 * i), df[i], y);
+        for (int i = 0; i < D / 16; ++i) y = mma(L::rows(lds[t % S::kBuffers][1], ln, 32 * n, 16 * i), df[i], y);
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const int key = t * BN + 32 * n + 8 * (i / 4) + 4 * h + i % 4;
@@ -888,13 +940,18 @@ __global__ __launch_bounds__(NW * 64, (Plan<T, D>::kDqWaves)) void k_attention_d
   for (int d = 0; d < D / 32; ++d) g[d] = zero16();
   const int edge = a.causal ? seen_keys(a, e, r0) / BN : t1;
   bool found = false;
-  if (t0 < t1) load(t0, 0);
+  if (t0 < t1) {
+    load(t0, 0);
+    S::store(lds[0][0], hk);
+    S::store(lds[0][1], hv);
+  }
   wait_copies();
   for (int t = t0; t < t1; ++t) {
     ln.renew();
-    char* kt = lds[(t - t0) & 1][0];
-    const char* vt = lds[(t - t0) & 1][1];
-    if (t + 1 < t1) load(t + 1, (t + 1 - t0) & 1);
+    const int b = (t - t0) % S::kBuffers;
+    char* kt = lds[b][0];
+    const char* vt = lds[b][1];
+    if (t + 1 < t1) load(t + 1, S::kBuffers - 1 - b);
     if (t >= edge) found |= clean<T, D, BN, NT>(kt);
     if (t * BN < seen_max) {
 #pragma unroll
@@ -904,6 +961,7 @@ __global__ __launch_bounds__(NW * 64, (Plan<T, D>::kDqWaves)) void k_attention_d
         for (int i = 0; i < D / 16; ++i) x = mma(L::rows(kt, ln, 32 * n, 16 * i), qf[i], x);
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) y = mma(L::rows(vt, ln, 32 * n, 16 * i), df[i], y);
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int i = 0; i < 16; ++i)
           x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], c, -lse2)) * (y[i] - delta);
@@ -920,6 +978,14 @@ __global__ __launch_bounds__(NW * 64, (Plan<T, D>::kDqWaves)) void k_attention_d
 #pragma unroll
           for (int d = 0; d < D / 32; ++d) g[d] = mma(L::cols(kt, ln, 32 * n + 16 * j, 32 * d), sf, g[d]);
         }
+        __builtin_amdgcn_s_setprio(0);
+      }
+    }
+    if constexpr (!S::kDirect) {
+      __syncthreads();
+      if (t + 1 < t1) {
+        S::store(lds[0][0], hk);
+        S::store(lds[0][1], hv);
       }
     }
     wait_copies();
@@ -946,7 +1012,8 @@ template <class T, int D, int NW, int BQ>
 __global__ __launch_bounds__(NW * 64, (Plan<T, D>::kDkvWaves)) void k_attention_dkv(AttnArgs a) {
   using L = Tile<T, D, BQ>;
   constexpr int NT = NW * 64, BK = NW * 32;
-  __shared__ __attribute__((aligned(16))) char lds[2][2][L::kBytes];
+  using S = Stage<T, D, BQ, NT>;
+  __shared__ __attribute__((aligned(16))) char lds[S::kBuffers][2][L::kBytes];
   __shared__ __attribute__((aligned(16))) float stat[2][2][BQ];
   using LK = Tile<T, D, BK>;
   constexpr bool kLds = Plan<T, D>::kValuesInLds;
@@ -988,12 +1055,13 @@ __global__ __launch_bounds__(NW * 64, (Plan<T, D>::kDkvWaves)) void k_attention_
   const float c = a.scale * kLog2e;
   constexpr float kUp = (float)(1 << Frag<T>::kShift), kDown = 1.f / kUp;
 
-  const Stage<T, D, BQ, NT> stage;
+  const S stage;
+  typename S::Held hq, hd;
   float ss = 0.f, sd = 0.f;
   const T* dout = (const T*)a.dout + at0 * a.dim;
   const auto load = [&](int t, int b) {
     stage.copy_packed(
-        lds[b][0], lds[b][1], a, t * BQ, rows,
+        lds[b][0], hq, lds[b][1], hd, a, t * BQ, rows,
         [&](int i, int g) { return q + ((uint64_t)(uint32_t)i * (uint32_t)a.q_row + (uint64_t)(uint32_t)g * (uint32_t)a.q_head); },
         [&](int i, int g) { return dout + (uint64_t)(uint32_t)(i * a.heads + g) * (uint32_t)a.dim; });
     if (threadIdx.x < BQ) {
@@ -1003,13 +1071,18 @@ __global__ __launch_bounds__(NW * 64, (Plan<T, D>::kDkvWaves)) void k_attention_
       sd = r < rows ? a.delta[at] * kDown : 0.f;
     }
   };
-  const auto store = [&](int b) {
+  const auto store_stats = [&](int b) {
     if (threadIdx.x < BQ) {
       stat[b][0][threadIdx.x] = ss;
       stat[b][1][threadIdx.x] = sd;
     }
   };
-  if constexpr (kLds) Stage<T, D, BK, NT>().copy(vt, v + j0 * a.v_row, a.v_row, e.lk - j0, a.dim);
+  if constexpr (kLds) {
+    using SK = Stage<T, D, BK, NT>;
+    typename SK::Held hv;
+    SK().copy(vt, hv, v + j0 * a.v_row, a.v_row, e.lk - j0, a.dim);
+    SK::store(vt, hv);
+  }
 #pragma unroll
   for (int d = 0; d < D / 32; ++d) gk[d] = gv[d] = zero16();
   // Rows before this one do not see all keys of the workgroup.
@@ -1017,7 +1090,9 @@ __global__ __launch_bounds__(NW * 64, (Plan<T, D>::kDkvWaves)) void k_attention_
   bool found = false;
   if (t0 < t1) {
     load(t0, 0);
-    store(0);
+    S::store(lds[0][0], hq);
+    S::store(lds[0][1], hd);
+    store_stats(0);
   }
   wait_copies();
   typename L::Lanes ln;
@@ -1025,10 +1100,10 @@ __global__ __launch_bounds__(NW * 64, (Plan<T, D>::kDkvWaves)) void k_attention_
   for (int t = t0; t < t1; ++t) {
     ln.renew();
     lk.renew();
-    const int b = (t - t0) & 1;
-    char* qt = lds[b][0];
-    char* dt = lds[b][1];
-    if (t + 1 < t1) load(t + 1, (t + 1 - t0) & 1);
+    const int b = (t - t0) & 1, at = b % S::kBuffers;
+    char* qt = lds[at][0];
+    char* dt = lds[at][1];
+    if (t + 1 < t1) load(t + 1, S::kBuffers - 1 - at);
     if ((int64_t)t * BQ < edge) {
       found |= clean<T, D, BQ, NT>(qt);
       found |= clean<T, D, BQ, NT>(dt);
@@ -1053,6 +1128,7 @@ __global__ __launch_bounds__(NW * 64, (Plan<T, D>::kDkvWaves)) void k_attention_
         pace<0, kLds ? D / 16 - 2 : D / 16 - 4, kLds ? 2 : 1, kLds ? 2 : 4>();
       }
       if constexpr (D > 32) __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_setprio(1);
       const int rn = t * BQ + 32 * n;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -1082,8 +1158,16 @@ __global__ __launch_bounds__(NW * 64, (Plan<T, D>::kDkvWaves)) void k_attention_
 #pragma unroll
         for (int d = 0; d < D / 32; ++d) gk[d] = mma(L::cols(qt, ln, 32 * n + 16 * j, 32 * d), sf, gk[d]);
       }
+      __builtin_amdgcn_s_setprio(0);
     }
-    if (t + 1 < t1) store((t + 1 - t0) & 1);
+    if (t + 1 < t1) store_stats(1 - b);
+    if constexpr (!S::kDirect) {
+      __syncthreads();
+      if (t + 1 < t1) {
+        S::store(lds[0][0], hq);
+        S::store(lds[0][1], hd);
+      }
+    }
     wait_copies();
   }
   if (found) {
@@ -1165,10 +1249,11 @@ static int parts_of(int64_t workgroups, int64_t wanted, int64_t steps, int64_t l
 // The device holds two workgroups per CU.  Parts cost a write and a read of
 // float rows each, so in 16 bits only grids under half of the device are split;
 // 32-bit steps take six times as long and are worth it up to all of it (8192
-// rows causal, 4 heads of 32: 276 us in one part, 134 in four).  Single steps
-// are not (937 rows, 4 heads of 64 over 2: 29 us in double steps, 37 in single
-// X and even out the
-// lengths (32 sequences of up to 8192 keys: 302 us in one part, 135 in eight).
+// rows causal, 4 heads of 32: 227 us in one part, 111 in four).  Single steps
+// are not (937 rows, 4 heads of 64 over 2: 27 us in double steps, 32 in single
+// ones).  Sequences whose rows fit one wave (single tokens) only stream their
+// keys: many short parts keep the loads going and even out the lengths (32
+// sequences of up to 8192 keys: 302 us in one part, 135 in eight).
 static int row_parts(int64_t workgroups, int64_t steps, int dtype) {
   if (dtype == kF32) return workgroups > 512 ? 1 : parts_of(workgroups, 1024, steps, 2);
   return workgroups > 256 ? 1 : parts_of(workgroups, 512, steps, 2);
