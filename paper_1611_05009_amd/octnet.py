@@ -768,27 +768,30 @@ def label_logprobs_backward(logits: torch.Tensor, labels: torch.Tensor, lse: tor
     return out
 
 
+def _clip_list(tensors):
+    """Types and sizes."""
+    kinds = [_TYPES.get(t.dtype) for t in tensors]
+    if None in kinds or not all([t.is_cuda and t.is_contiguous() for t in tensors]):
+        raise OctNetError("the gradients must be contiguous GPU tensors of float32, float16 or bfloat16")
+    return kinds, [t.numel() for t in tensors]
+
+
 def clip_grad_norm(grads, max_norm: float, out=None, ws: torch.Tensor | None = None) -> torch.Tensor:
-    """Scales the gradients (a list of GPU tensors, of any of the three types) by min(1, max_norm / (norm + 1e-6)), in place or into `out`, and
-    returns their common norm, a float32 scalar on the GPU (nothing waits for
-    it)."""
-    src, count, kind = array.array("Q"), array.array("q"), array.array("i")
-    for t in grads:
-        if t.dtype not in _TYPES or not t.is_cuda or not t.is_contiguous():
-            raise OctNetError("the gradients must be contiguous GPU tensors of float32, float16 or bfloat16")
-        src.append(t.data_ptr())
-        count.append(t.numel())
-        kind.append(_TYPES[t.dtype])
-    n = len(src)
+    """Scales the gradients (a list of GPU tensors, of any of the three types)
+    by min(1, max_norm / (norm + 1e-6)), in place or into `out`, and returns
+    their common norm, a float32 scalar on the GPU (nothing waits for it)."""
+    grads = list(grads)
+    n = len(grads)
+    kinds, counts = _clip_list(grads)
+    src = array.array("Q", [t.data_ptr() for t in grads])
     dst = src
     if out is not None:
-        dst = array.array("Q", [o.data_ptr() for o in out])
-        if len(dst) != n:
+        out = list(out)
+        if len(out) != n or _clip_list(out) != (kinds, counts):
             raise OctNetError("out must match the gradients")
-        for o, c, k in zip(out, count, kind):
-            if o.numel() != c or _TYPES.get(o.dtype) != k or not o.is_cuda or not o.is_contiguous():
-                raise OctNetError("out must match the gradients")
-    norm = torch.empty((), dtype=torch.float32, device=_dev() if n == 0 else t.device)
+        dst = array.array("Q", [t.data_ptr() for t in out])
+    count, kind = array.array("q", counts), array.array("i", kinds)
+    norm = torch.empty((), dtype=torch.float32, device=_dev() if n == 0 else grads[0].device)
     counts, types = count.buffer_info()[0], kind.buffer_info()[0]
     if ws is None:
         nb = ctypes.c_size_t(0)
