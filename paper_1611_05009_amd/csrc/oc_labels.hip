@@ -12,7 +12,7 @@
 // where rows are few, each with running statistics per lane.
 //
 // The top alternatives of a streamed row come from lists: each wave appends
-// what exceeds the least of its best `top` values so far, which after the
+// what exceeds a bound of the row's `top` best values so far, which after the
 // first few hundred elements is rare, and shrinks its list to the best
 // whenever it fills.  A wave meets its elements in ascending order, so that an
 // equal value met later is rightly left out: ties go to the lowest index.
@@ -28,7 +28,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 #define OC_INF __builtin_inff()
 constexpr int kNone = 0x7fffffff;   // index of no element
-constexpr int kCap = 1024;          // entries of a wave's list
+constexpr int kCap = 640;           // entries of a wave's list: 95 and those of a step
 constexpr int kStep = 512;          // elements that a wave takes at a time
 
 __device__ __forceinline__ int lane() { return (int)(threadIdx.x & 63); }
@@ -274,14 +274,21 @@ struct List {
     count += __popcll(all);
   }
 
-  // Bounds the first elements: of every lane's greatest, x, the `top`-th is no
-  // better than the `top`-th of all.
-  __device__ __forceinline__ void start(float x, int top) {
-    const float k = kth(x, top);
+  // Bounds what is to come: of every lane's greatest so far, x, the `top`-th is
+  // no better than the `top`-th of all.  That holds for the whole row, so the
+  // waves share their bounds in LDS; each keeps what equals them, and whenever
+  // a wave gets to see another's bound, the best of all lists stay the same.
+  // (1021 rows of 100003, 8 alternatives: one bound from the first step 62 us,
+  // shared and renewed 58; 1 alternative 58 and 52.)
+  __device__ __forceinline__ void bound(float x, int top, volatile float* bounds, int w) {
+    const float k = kth<16>(x, top);
     const int b = (int)__float_as_uint(k);
     // The next lower number, so that equal ones enter.
-    least = k == -OC_INF ? k : __uint_as_float(k > 0.f ? b - 1 : k < 0.f ? b + 1 : 0x80000001);
-    next = 64 + top;
+    const float below = k > -OC_INF ? __uint_as_float(k > 0.f ? b - 1 : k < 0.f ? b + 1 : 0x80000001) : -OC_INF;
+    if (lane() == 0) bounds[w] = below;
+    least = fmaxf(least, below);
+#pragma unroll
+    for (int o = 0; o < 4; ++o) least = fmaxf(least, bounds[o]);
   }
 
   // Keeps the list's `top` best (at most 32), in order, at its front.
@@ -317,7 +324,7 @@ struct List {
       float bound;
       int bound_j = kNone;
       if (!equal) {
-        bound = kth(best, top);
+        bound = kth<32>(best, top);
       } else {
         const int l = __ffsll((unsigned long long)__ballot(place(best, best_j, 64) == top - 1)) - 1;
         bound = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(best), l));
@@ -348,11 +355,13 @@ struct List {
     next = 64 + top;
   }
 
-  // The k-th greatest of the lanes' x, bit by bit; NaN counts as -infinity.
+  // The k-th greatest of the lanes' x, bit by bit, or of its upper BITS the
+  // least number that has them; NaN counts as -infinity.
+  template <int BITS>
   static __device__ __forceinline__ float kth(float x, int k) {
     const uint32_t b = __float_as_uint(x == x ? x + 0.f : -OC_INF), key = b ^ ((uint32_t)((int)b >> 31) | 0x80000000u);  // same order
     uint32_t r = 0;
-    for (int i = 31; i >= 0; --i) {
+    for (int i = 31; i > 31 - BITS; --i) {
       const uint32_t up = r | (1u << i);
       if (__popcll(__ballot(key >= up)) >= k) r = up;
     }
@@ -402,6 +411,14 @@ __device__ __forceinline__ void finish_top(const LabelArgs& a, int64_t row, cons
   if (lane() >= count && lane() < a.top) write_top(a, row, lane(), 0.f, kNone, st);
 }
 
+
+// Eight elements of a slot: 16 bytes, or 32 in two halves 1024 bytes apart.
+template <class T>
+__device__ __forceinline__ f32x8 from_ring(const char* p) {
+  if constexpr (sizeof(T) == 2) return __builtin_convertvector(*(const typename Vec8<T>::type*)p, f32x8);
+  else return __builtin_shufflevector(*(const f32x4*)p, *(const f32x4*)(p + 1024), 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
 // One workgroup per row (blockIdx.x) and part of it (blockIdx.y).  Writes the
 // row's results, or where a row has several parts their statistics and lists.
 template <class T, bool TOP>
@@ -413,8 +430,16 @@ __global__ __launch_bounds__(256) void k_labels_streamed(LabelArgs a) {
   const int j0 = (int)blockIdx.y * a.per, j1 = j0 + a.per < a.classes ? j0 + a.per : a.classes;
   const T* x = (const T*)a.logits + row * a.classes + j0;
   const int n = j1 - j0, head = head_of(x, n), body = (n - head) / 8, w = wave();
-  List list{vals + (TOP ? w * kCap : 0), idxs + (TOP ? w * kCap : 0), 0, 0, -OC_INF};
+  List list{vals + (TOP ? w * kCap : 0), idxs + (TOP ? w * kCap : 0), 0, 64 + a.top, -OC_INF};
   Stat st;
+  // Greatest element of each lane; its bound is renewed after 1, 2, 4, .. steps.
+  float most = -OC_INF;
+  uint32_t steps = 0;
+  __shared__ float bounds[4];
+  if (TOP) {
+    if (lane() == 0) bounds[w] = -OC_INF;
+    __syncthreads();
+  }
 
   const auto one = [&](bool in, int j) {
     const float y = in ? (float)x[j] : -OC_INF;
@@ -423,24 +448,37 @@ __global__ __launch_bounds__(256) void k_labels_streamed(LabelArgs a) {
     if (TOP) list.push(in && y > list.least, y, j0 + j);
   };
   if (w == 0 && head) one(lane() < head, lane());
-  // Two vectors per lane are on their way while one is worked on.  The loop
-  // is not unrolled: its list handling would not fit the instruction cache.
-  using Raw = typename Vec8<T>::type;
+  // Vectors come by asynchronous copies into a ring in LDS, of which all slots
+  // but one are on their way while that one is worked on.  (Held in registers,
+  // the next vectors were waited for as soon as they moved on by a place: 1021
+  // rows of 100003 in bfloat16, without and with 8 alternatives, 46 and 66 us, so
+  // 41 and 62.)  The loop is not unrolled: its list handling would not fit the
+  // instruction cache.
+  constexpr int kLoads = sizeof(T) / 2, kSlots = 4 / kLoads;
+  __shared__ __attribute__((aligned(16))) char ring[4][kSlots][kLoads][1024];
   const T* from = x + head;
-  const auto fetch = [&](int v0, Raw& r) {
-    const int v = v0 + lane();
-    if (v < body) r = *(const Raw*)(from + 8 * (int64_t)v);
+  const auto fetch = [&](int v0) {
+    // Past the end the last vector once more: no slot is left out.
+    const int v = v0 + lane() < body ? v0 + lane() : body - 1;
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k) {
+      const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)ring[w][v0 / 256 % kSlots][k];
+      // It writes no register; vmcnt waits for it.
+      asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"{m0}"(to),
+                   "v"((const char*)(from + 8 * (int64_t)v) + 16 * k)
+                   : "memory");
+    }
   };
-  Raw r0 = {}, r1 = {}, r2 = {};
-  fetch(64 * w, r0);
-  fetch(64 * w + 256, r1);
+  if (64 * w < body) {
+#pragma unroll
+    for (int k = 0; k < kSlots - 1; ++k) fetch(64 * w + 256 * k);
+  }
 #pragma unroll 1
   for (int v0 = 64 * w; v0 < body; v0 += 256) {
-    fetch(v0 + 512, r2);
+    fetch(v0 + 256 * (kSlots - 1));
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((kSlots - 1) * kLoads) : "memory");
     const int v = v0 + lane();
-    f32x8 y = __builtin_convertvector(r0, f32x8);
-    r0 = r1;
-    r1 = r2;
+    f32x8 y = from_ring<T>(ring[w][v0 / 256 % kSlots][0] + lane() * 16);
     if (v >= body) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) y[i] = -OC_INF;
@@ -452,7 +490,9 @@ __global__ __launch_bounds__(256) void k_labels_streamed(LabelArgs a) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) st.add(y[i]);
     if constexpr (TOP) {
-      if (list.next == 0) list.start(top, a.top);
+      most = fmaxf(most, top);
+      if ((steps & (steps + 1)) == 0) list.bound(most, a.top, bounds, w);
+      ++steps;
       if (__ballot(top > list.least)) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -463,6 +503,7 @@ __global__ __launch_bounds__(256) void k_labels_streamed(LabelArgs a) {
       }
     }
   }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   // The last wave takes the elements past the last whole vector.
   const int tail = head + 8 * body;
   if (w == 3 && tail < n) one(tail + lane() < n, tail + lane());
@@ -528,7 +569,7 @@ __global__ __launch_bounds__(64) void k_labels_join(LabelArgs a) {
   st = group_stat(st, 64);
   if (lane() == 0) write_row(a, row, st, label_logit<T>(a, row));
   if constexpr (TOP) {
-    List list{vals, idxs, 0, 0, -OC_INF};
+    List list{vals, idxs, 0, 64 + a.top, -OC_INF};
     const int n = a.parts * a.top;
     for (int e = 0; e < n; e += 64) {
       if (list.count > kCap - 64) list.shrink(a.top);
