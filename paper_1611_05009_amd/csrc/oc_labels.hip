@@ -368,14 +368,18 @@ struct List {
     return __uint_as_float(r ^ ((uint32_t)((int)~r >> 31) | 0x80000000u));
   }
 
-  // How many of the first n lanes hold something better than this one.
+  // How many of the first n lanes hold something better than this one.  As one
+  // comparison of 64 bits: the value in their order, then the index from above.
   static __device__ __forceinline__ int place(float x, int j, int n) {
+    const uint32_t b = __float_as_uint(x + 0.f), hi = b ^ ((uint32_t)((int)b >> 31) | 0x80000000u), lo = ~(uint32_t)j;
+    const uint64_t mine = (uint64_t)hi << 32 | lo;
     int r = 0;
     for (int l = 0; l < n; l += 8)  // lanes past the n-th hold nothing better
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        const float y = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), l + k));
-        r += better(y, __builtin_amdgcn_readlane(j, l + k), x, j) ? 1 : 0;
+        const uint64_t y = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(hi, l + k) << 32 |
+                           (uint32_t)__builtin_amdgcn_readlane(lo, l + k);
+        r += y > mine ? 1 : 0;
       }
     return r;
   }
