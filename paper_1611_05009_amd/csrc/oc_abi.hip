@@ -708,7 +708,8 @@ int oc_attention_workspace(int64_t n_q, int64_t n_k, int n_seq, int heads, int k
   const int rc = attention_sizes("oc_attention_workspace", n_q, n_k, n_seq, heads, kv_heads, dim);
   if (rc != OC_OK) return rc;
   if (!type_ok(dtype)) return fail(OC_EINVAL, "oc_attention_workspace: bad type %d", dtype);
-  const int n = oci::attention_splits(n_q, n_k, n_seq, heads, kv_heads, dtype);
+  // Causal calls take as many parts as others, or more.
+  const int n = oci::attention_splits(n_q, n_k, n_seq, heads, kv_heads, dtype, true);
   const size_t rows = (size_t)n_q * heads;
   *bytes = n > 1 ? oci::align256(4 * n * rows * dim) + oci::align256(4 * n * rows) : 0;
   return OC_OK;
@@ -730,7 +731,7 @@ int oc_attention(const void* q, int64_t q_row, int64_t q_head, const void* k, in
   a.k_len = k_len;
   a.out = out;
   a.lse = lse;
-  a.n_split = oci::attention_splits(n_q, n_k, n_seq, heads, kv_heads, dtype);
+  a.n_split = oci::attention_splits(n_q, n_k, n_seq, heads, kv_heads, dtype, causal != 0);
   if (a.n_split > 1) {
     const size_t rows = (size_t)n_q * heads, part = oci::align256(4 * a.n_split * rows * dim);
     if (!ws || ws_bytes < part + oci::align256(4 * a.n_split * rows))
@@ -751,7 +752,7 @@ int oc_attention_backward_workspace(int64_t n_q, int64_t n_k, int n_seq, int hea
   if (rc != OC_OK) return rc;
   if (!type_ok(dtype)) return fail(OC_EINVAL, "oc_attention_backward_workspace: bad type %d", dtype);
   *bytes = 2 * oci::align256(4 * (size_t)n_q * heads) +
-           oci::attention_back_parts(n_q, n_k, n_seq, heads, kv_heads, dim, dtype).bytes;
+           oci::attention_back_parts(n_q, n_k, n_seq, heads, kv_heads, dim, dtype, true).bytes;
   return OC_OK;
 }
 
@@ -771,7 +772,8 @@ int oc_attention_backward(const void* q, int64_t q_row, int64_t q_head, const vo
   if (!aligned16(out) || !aligned16(dout) || !aligned16(dq) || !aligned16(dk) || !aligned16(dv))
     return fail(OC_EINVAL, "oc_attention_backward: pointer not aligned to 16 bytes");
   const size_t part = oci::align256(4 * (size_t)n_q * heads);
-  const size_t need = 2 * part + oci::attention_back_parts(n_q, n_k, n_seq, heads, kv_heads, dim, dtype).bytes;
+  const size_t need = 2 * part +
+                      oci::attention_back_parts(n_q, n_k, n_seq, heads, kv_heads, dim, dtype, causal != 0).bytes;
   if (need && (!ws || ws_bytes < need)) return fail(OC_EWORKSPACE, "oc_attention_backward: workspace too small");
   if (!aligned16(ws)) return fail(OC_EINVAL, "oc_attention_backward: workspace not aligned to 16 bytes");
   a.out = const_cast<void*>(out);

@@ -31,7 +31,8 @@ struct AttnArgs {
 // Fills group and its division from heads and kv_heads.
 void attention_set_group(AttnArgs* a);
 // Parts into which the keys of each row tile are split.
-int attention_splits(int64_t n_q, int64_t n_k, int n_seq, int heads, int kv_heads, int dtype);
+int attention_splits(int64_t n_q, int64_t n_k, int n_seq, int heads, int kv_heads, int dtype,
+                     bool causal);
 hipError_t launch_attention(const AttnArgs& a, int dtype, hipStream_t s);
 // Parts of the gradients' kernels and the bytes that these take.
 struct AttnParts {
@@ -39,7 +40,7 @@ struct AttnParts {
   size_t bytes;
 };
 AttnParts attention_back_parts(int64_t n_q, int64_t n_k, int n_seq, int heads, int kv_heads, int dim,
-                               int dtype);
+                               int dtype, bool causal);
 hipError_t launch_attention_backward(AttnArgs a, int dtype, hipStream_t s);
 
 }  // namespace oci

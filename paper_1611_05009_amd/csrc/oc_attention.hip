@@ -1251,28 +1251,38 @@ static int parts_of(int64_t workgroups, int64_t wanted, int64_t steps, int64_t l
 }
 
 // The device holds two workgroups per CU.  Parts cost a write and a read of
-// float rows each, so in 16 bits only grids under half of the device are split;
-// 32-bit steps take six times as long and are worth it up to all of it (8192
-// rows causal, 4 heads of 32: 227 us in one part, 111 in four).  Single steps
-// are not (937 rows, 4 heads of 64 over 2: 27 us in double steps, 32 in single
-// ones).  Sequences whose rows fit one wave (single tokens) only stream their
-// keys: many short parts keep the loads going and even out the lengths (32
-// sequences of up to 8192 keys: 302 us in one part, 135 in eight).
-static int row_parts(int64_t workgroups, int64_t steps, int dtype) {
-  if (dtype == kF32) return workgroups > 512 ? 1 : parts_of(workgroups, 1024, steps, 2);
-  return workgroups > 256 ? 1 : parts_of(workgroups, 512, steps, 2);
+// float rows each, so in 16 bits grids under half of the device are split until
+// they fill it once.  Grids that fill it less than once, but more than half, run
+// as long as their longest tile: in three parts they even out where rows see
+// enough keys (us in one and three parts, forward: 8192 causal, 4 heads of 32: 80,
+// 46; 16384 causal, 2 of 128: 290, 169; 2048 causal, 16 of 64: 36, 32; 4096 of 8
+// of 64: 64, 57; but 1024 causal, 32 of 64: 22, 26; 2048, 16 of 128 over 4: 45, 62).
+// 32-bit steps take six times as long and are worth splitting up to all of the
+// device (8192 causal, 4 heads of 32: 227 us in one part, 111 in four).  Single
+// steps are not (937 rows, 4 heads of 64 over 2: 27 us in double steps, 32 in
+// single ones).
+static int row_parts(int64_t workgroups, int64_t steps, int dtype, bool causal) {
+  if (workgroups > 512) return 1;
+  if (dtype == kF32) return parts_of(workgroups, 1024, steps, 2);
+  if (workgroups <= 256) return parts_of(workgroups, 512, steps, 2);
+  return steps >= (causal ? 32 : 64) ? 3 : 1;
 }
 
-int attention_splits(int64_t n_q, int64_t n_k, int n_seq, int heads, int kv_heads, int dtype) {
+// Sequences whose rows fit one wave (single tokens) only stream their keys: many
+// short parts keep the loads going and even out the lengths (32 sequences of up
+// to 8192 keys: 302 us in one part, 135 in eight).
+int attention_splits(int64_t n_q, int64_t n_k, int n_seq, int heads, int kv_heads, int dtype, bool causal) {
   const int64_t rows = n_q * (heads / kv_heads), workgroups = slots_of(rows, kTile, n_seq) * kv_heads;
   const int64_t steps = n_k / n_seq / 64;
-  return rows <= 32 * (int64_t)n_seq ? parts_of(workgroups, 2048, steps, 2) : row_parts(workgroups, steps, dtype);
+  return rows <= 32 * (int64_t)n_seq ? parts_of(workgroups, 2048, steps, 2)
+                                     : row_parts(workgroups, steps, dtype, causal);
 }
 
-AttnParts attention_back_parts(int64_t n_q, int64_t n_k, int n_seq, int heads, int kv_heads, int dim, int dtype) {
+AttnParts attention_back_parts(int64_t n_q, int64_t n_k, int n_seq, int heads, int kv_heads, int dim, int dtype,
+                               bool causal) {
   AttnParts p;
   const int64_t rows = n_q * (heads / kv_heads);
-  p.dq = row_parts(slots_of(rows, kTile, n_seq) * kv_heads, n_k / n_seq / 64, dtype);
+  p.dq = row_parts(slots_of(rows, kTile, n_seq) * kv_heads, n_k / n_seq / 64, dtype, causal);
   // Causal tiles differ by far in their work; twice as many workgroups as the
   // device holds even it out (432 TFLOP/s with one part, 749 with two).
   p.dkv = parts_of(slots_of(n_k, kTile, n_seq) * kv_heads, 1024, rows / n_seq / 64, 2);
@@ -1302,7 +1312,7 @@ hipError_t launch_attention(const AttnArgs& a, int dtype, hipStream_t s) {
 }
 
 hipError_t launch_attention_backward(AttnArgs a, int dtype, hipStream_t s) {
-  const AttnParts parts = attention_back_parts(a.n_q, a.n_k, a.n_seq, a.heads, a.kv_heads, a.dim, dtype);
+  const AttnParts parts = attention_back_parts(a.n_q, a.n_k, a.n_seq, a.heads, a.kv_heads, a.dim, dtype, a.causal);
   const int64_t n_dq = a.n_q * a.heads * a.dim, n_dkv = a.n_k * a.kv_heads * a.dim;
   float* dq_part = a.part;
   float* dkv_part = a.part + (parts.dq > 1 ? parts.dq * n_dq : 0);
