@@ -1257,12 +1257,15 @@ static int parts_of(int64_t workgroups, int64_t wanted, int64_t steps, int64_t l
 // enough keys (us in one and three parts, forward: 8192 causal, 4 heads of 32: 80,
 // 46; 16384 causal, 2 of 128: 290, 169; 2048 causal, 16 of 64: 36, 32; 4096 of 8
 // of 64: 64, 57; but 1024 causal, 32 of 64: 22, 26; 2048, 16 of 128 over 4: 45, 62).
+// So do long causal ones that fill it up to twice, in two (16384, 4 of 128: 373,
+// 296; 8192, 8 of 64: 129, 105; 12000, 8 of 96: 279, 286; but 6000, 16 of 64: 111,
+// 115; 3000, 32 of 128 over 8: 89, 115).
 // 32-bit steps take six times as long and are worth splitting up to all of the
 // device (8192 causal, 4 heads of 32: 227 us in one part, 111 in four).  Single
 // steps are not (937 rows, 4 heads of 64 over 2: 27 us in double steps, 32 in
 // single ones).
 static int row_parts(int64_t workgroups, int64_t steps, int dtype, bool causal) {
-  if (workgroups > 512) return 1;
+  if (workgroups > 512) return causal && workgroups <= 1024 && steps >= 96 && dtype != kF32 ? 2 : 1;
   if (dtype == kF32) return parts_of(workgroups, 1024, steps, 2);
   if (workgroups <= 256) return parts_of(workgroups, 512, steps, 2);
   return steps >= (causal ? 32 : 64) ? 3 : 1;
