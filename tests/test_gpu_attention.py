@@ -333,3 +333,24 @@ def test_long_cache_past_32_bits():
     near(out[1:], w[0], w[2] + 4 * U32 * w[0].abs(), "out")
     near(lse[1:], w[1], w[3] + 8 * U32, "lse")
     assert not out[0].any() and torch.allclose(lse[0], torch.full_like(lse[0], math.log(n - tail)), rtol=1e-5)
+
+
+@pytest.mark.parametrize("dtype,n,heads,dim,causal", [
+    (torch.bfloat16, 2049, 16, 24, True), (torch.float16, 4100, 8, 16, False), (torch.bfloat16, 6200, 11, 8, True),
+    (torch.float32, 3001, 11, 16, True)])
+def test_grids_near_the_device(dtype, n, heads, dim, causal):
+    """Grids of once or twice the workgroups that the device holds, whose tiles
+    are taken in parts; the first and the last head are checked."""
+    from paper_1611_05009_amd import octnet as oc
+    q, k, v, d = inputs(11, dtype, n, n, heads, heads, dim)
+    out, lse = oc.attention(q, k, v, causal=causal)
+    grads = oc.attention_backward(q, k, v, out, lse, d, causal=causal)
+    torch.cuda.synchronize()
+    for h in (0, heads - 1):
+        one = slice(h, h + 1)
+        w = reference(q[:, one], k[:, one], v[:, one], [0, n], [0, n], None, causal, dim ** -0.5, UNIT[dtype], TINY[dtype],
+                      d[:, one])
+        near(out[:, one], w[0], w[2], "out")
+        near(lse[:, one], w[1], w[3], "lse")
+        for i, name in enumerate(("dq", "dk", "dv")):
+            near(grads[i][:, one], w[4][i], w[4][3 + i], name)
