@@ -1290,7 +1290,9 @@ static int parts_of(int64_t workgroups, int64_t wanted, int64_t steps, int64_t l
 
 // The device holds two workgroups per CU.  Parts cost a write and a read of
 // float rows each, so in 16 bits grids under half of the device are split until
-// they fill it once.  Grids that fill it less than once, but more than half, run
+// they fill it once; without a mask not far past it, where a few parts would run
+// by themselves at the end (3000 rows, 8 heads of 96: 61 us in three parts, 50 in
+// two).  Grids that fill it less than once, but more than half, run
 // as long as their longest tile: in three parts they even out where rows see
 // enough keys (us in one and three parts, forward: 8192 causal, 4 heads of 32: 80,
 // 46; 16384 causal, 2 of 128: 290, 169; 2048 causal, 16 of 64: 36, 32; 4096 of 8
@@ -1305,7 +1307,10 @@ static int parts_of(int64_t workgroups, int64_t wanted, int64_t steps, int64_t l
 static int row_parts(int64_t workgroups, int64_t steps, int dtype, bool causal) {
   if (workgroups > 512) return causal && workgroups <= 1024 && steps >= 96 && dtype != kF32 ? 2 : 1;
   if (dtype == kF32) return parts_of(workgroups, 1024, steps, 2);
-  if (workgroups <= 256) return parts_of(workgroups, 512, steps, 2);
+  if (workgroups <= 256) {
+    const int n = parts_of(workgroups, 512, steps, 2);
+    return !causal && n * workgroups > 560 ? n - 1 : n;
+  }
   return steps >= (causal ? 32 : 64) ? 3 : 1;
 }
 
@@ -1326,7 +1331,11 @@ AttnParts attention_back_parts(int64_t n_q, int64_t n_k, int n_seq, int heads, i
   p.dq = row_parts(slots_of(rows, kTile, n_seq) * kv_heads, n_k / n_seq / 64, dtype, causal);
   // Causal tiles differ by far in their work; twice as many workgroups as the
   // device holds even it out (432 TFLOP/s with one part, 749 with two).
-  p.dkv = parts_of(slots_of(n_k, kTile, n_seq) * kv_heads, 1024, rows / n_seq / 64, 2);
+  // Many parts keep below that (3000 rows, 8 heads of 96, all gradients: 172 us in six,
+  // 155 in five), few go past it (8 causal sequences of up to 4099 rows, 16 heads
+  // of 128 over 4: dK and dV 430 us in three, 515 in two).
+  const int64_t workgroups = slots_of(n_k, kTile, n_seq) * kv_heads;
+  p.dkv = parts_of(workgroups, workgroups <= 256 ? 1024 / workgroups * workgroups : 1024, rows / n_seq / 64, 2);
   const int64_t a = p.dq > 1 ? p.dq * n_q * heads : 0, b = p.dkv > 1 ? 2 * p.dkv * n_k * kv_heads : 0;
   p.bytes = (size_t)(a + b) * dim * sizeof(float);
   return p;
