@@ -354,3 +354,37 @@ def test_grids_near_the_device(dtype, n, heads, dim, causal):
         near(lse[:, one], w[1], w[3], "lse")
         for i, name in enumerate(("dq", "dk", "dv")):
             near(grads[i][:, one], w[4][i], w[4][3 + i], name)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
+def test_attention_in_a_graph(dtype):
+    """Captured with its gradients and replayed on other inputs, with eager work
+    between the replays: the eager call's bits each time."""
+    from paper_1611_05009_amd import octnet as oc
+    lens = [300, 0, 517, 64]
+    off = offsets(lens)
+    kw = dict(q_offsets=off, k_offsets=off, causal=True)
+    q, k, v, d = inputs(21, dtype, sum(lens), sum(lens), 4, 2, 40)
+
+    def step():
+        out, lse = oc.attention(q, k, v, **kw)
+        return (out, lse) + tuple(oc.attention_backward(q, k, v, out, lse, d, **kw))
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        held = step()
+    for seed in range(4):
+        for t, u in zip((q, k, v, d), inputs(30 + seed, dtype, sum(lens), sum(lens), 4, 2, 40)):
+            t.copy_(u)
+        g.replay()
+        got = [t.clone() for t in held]
+        torch.cuda.synchronize()
+        want = step()
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
