@@ -133,7 +133,7 @@ def _ptr(t):
         raise OctNetError("expected a GPU tensor")
     if not t.is_contiguous():
         raise OctNetError("expected a contiguous tensor")
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
 def _stream():
@@ -560,12 +560,12 @@ def _heads(t: torch.Tensor, what: str):
         raise OctNetError("expected a GPU tensor")
     if t.dim() != 3:
         raise OctNetError("%s must be [rows, heads, dim]" % what)
-    if t.numel() and t.shape[2] > 1 and t.stride(2) != 1:
+    n, h, d = t.shape
+    rows, heads, one = t.stride()
+    if one != 1 and d > 1 and t.numel():
         raise OctNetError("%s must be contiguous along dim" % what)
     # The stride of an axis of one place is never used.
-    rows = t.stride(0) if t.shape[0] > 1 else 0
-    heads = t.stride(1) if t.shape[1] > 1 else 0
-    return ctypes.c_void_p(t.data_ptr()), rows, heads
+    return t.data_ptr(), rows if n > 1 else 0, heads if h > 1 else 0
 
 
 def _offsets(t: torch.Tensor | None, n: int, what: str):
