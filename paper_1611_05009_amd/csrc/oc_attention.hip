@@ -281,7 +281,8 @@ struct Stage {
   static __device__ __forceinline__ void put(char* t, Held& held, int i, const T* p) {
     if (!p) p = (const T*)kZeros;
     if constexpr (!kDirect) {
-      held.x[i] = *(const f32x8*)p;
+      const f32x4 x = *(const f32x4*)p, y = *(const f32x4*)(p + 4);
+      held.x[i] = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
       return;
     }
     char* to = t + (wave() + i * (NT / 64)) * (1024 + L::kPad);
