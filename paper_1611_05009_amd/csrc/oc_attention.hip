@@ -309,7 +309,9 @@ struct Stage {
   // R rows from p on, `stride` elements apart, of which `rows` exist.
   __device__ __forceinline__ void copy(char* t, Held& held, const T* p, int64_t stride, int rows, int dim) const {
     const T* q = p + row * stride;
-    if (rows >= R && dim == D) {
+    // Unchecked only where the head fills the tile's rows: one of 96 lies in rows of
+    // 128, whose last places are beyond the row in memory, and beyond the last one's end.
+    if (rows >= R && dim == L::P) {
 #pragma unroll
       for (int i = 0; i < kN; ++i) put(t, held, i, q + i * kStep * stride + col(i));
     } else {
